@@ -22,10 +22,15 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libquest.so")
 
 QUEST_F32, QUEST_BF16 = 0, 1
+QUEST_MX_E2M1, QUEST_MX_E4M3 = 0, 1
+QUEST_MX_GROUP = 32
 EXPORTS = ("quest_hadamard_quantize", "quest_hadamard_quantize_pair", "quest_hadamard_quantize_absmax", "quest_hadamard_quantize_fp4", "quest_hadamard_quantize_fp4_pair", "quest_alpha_star_fp4",
            "quest_lowbit_gemm", "quest_lowbit_gemm_workspace_bytes", "quest_lowbit_gemm_static", "quest_lowbit_gemm_fp4", "quest_trust_backward", "quest_trust_backward_pair",
            "quest_grad_gemm", "quest_grad_gemm_workspace_bytes", "quest_grad_gemm_fp4",
            "quest_grad_gemm_fp4_workspace_bytes", "quest_weight_only_gemm", "quest_weight_only_gemm_workspace_bytes",
+           "quest_hadamard_quantize_mx", "quest_dequantize_mx", "quest_lowbit_gemm_mx", "quest_grad_gemm_mx",
+           "quest_grad_gemm_mx_workspace_bytes", "quest_rms_norm_mx", "quest_rms_norm_backward",
+           "quest_rms_norm_backward_workspace_bytes",
            "quest_init", "quest_alpha_star", "quest_container_bits", "quest_status_string")
 
 _i64, _i32, _f32, _p = ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p
@@ -83,6 +88,20 @@ def load():
             getattr(lib, name).restype = _i64
         lib.quest_weight_only_gemm_workspace_bytes.argtypes = [_i64, _i64, _i64]
         lib.quest_weight_only_gemm_workspace_bytes.restype = _i64
+        lib.quest_hadamard_quantize_mx.argtypes = [_p, _i32, _i64, _i64, _i64, _i32, _i32, _p, _p, _p, _p]
+        lib.quest_dequantize_mx.argtypes = [_p, _p, _i32, _i64, _i64, _p, _i32, _i64, _p]
+        lib.quest_lowbit_gemm_mx.argtypes = [_p, _p, _i32, _i64, _p, _p, _i64, _i64, _p, _i64, _p, _p]
+        lib.quest_grad_gemm_mx.argtypes = [_i32, _p, _p, _p, _i32, _i64, _i64, _i64, _p, _p, _i64, _p]
+        lib.quest_rms_norm_mx.argtypes = [_p, _i64, _p, _i64, _i32, _p, _i32, _i64, _i64, _f32, _p, _p, _i32, _i32, _p, _p, _p,
+                                          _p, _p]
+        lib.quest_rms_norm_backward.argtypes = [_p, _p, _i32, _p, _i32, _p, _p, _i64, _i64, _p, _p, _p, _i64, _p]
+        for name in ("quest_hadamard_quantize_mx", "quest_dequantize_mx", "quest_lowbit_gemm_mx", "quest_grad_gemm_mx",
+                     "quest_rms_norm_mx", "quest_rms_norm_backward"):
+            getattr(lib, name).restype = ctypes.c_int
+        lib.quest_grad_gemm_mx_workspace_bytes.argtypes = [_i32, _i64, _i64, _i64]
+        lib.quest_grad_gemm_mx_workspace_bytes.restype = _i64
+        lib.quest_rms_norm_backward_workspace_bytes.argtypes = [_i64, _i64]
+        lib.quest_rms_norm_backward_workspace_bytes.restype = _i64
         lib.quest_init.argtypes = []
         lib.quest_init.restype = ctypes.c_int
         for name in ("quest_hadamard_quantize", "quest_hadamard_quantize_absmax", "quest_lowbit_gemm",
@@ -376,3 +395,138 @@ def quest_weight_only_gemm(x: torch.Tensor, w_codes: torch.Tensor, w_scales: tor
                                                _ptr(workspace), _bytes(workspace), _stream())
     if status:
         raise QuestError(status, "quest_weight_only_gemm")
+
+
+# ---- microscaled operands and the norm in front of them; these calls check what the pointers they pass stand for
+
+def _current_device() -> int:
+    return torch.cuda.current_device() if _device is None else _device()
+
+
+def _check_devices(*tensors: torch.Tensor | None) -> None:
+    here = _current_device()
+    for t in tensors:
+        if t is not None and (t.device.type != "cuda" or t.device.index != here):
+            raise ValueError(f"a tensor is on {t.device}, the call runs on cuda:{here}")
+
+
+def _rows(t: torch.Tensor, name: str, cols: int | None = None, rows: int | None = None):
+    """(rows, cols, row stride) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (cols is not None and t.shape[1] != cols) or (rows is not None and t.shape[0] != rows):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{'rows' if rows is None else rows}, "
+                         f"{'cols' if cols is None else cols}]")
+    if t.stride(1) != 1 and t.shape[1] != 1:
+        raise ValueError(f"{name}: the elements of a row are not contiguous")
+    return t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _packed(t: torch.Tensor | None, name: str, dtype: torch.dtype, shape: tuple) -> None:
+    """A contiguous tensor of exactly this shape, or None."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _code_bytes(fmt: int, cols: int) -> int:
+    if fmt not in (QUEST_MX_E2M1, QUEST_MX_E4M3):
+        raise ValueError(f"unknown format {fmt}")
+    return cols if fmt == QUEST_MX_E4M3 else cols // 2
+
+
+def _operand(codes: torch.Tensor | None, scales: torch.Tensor | None, mask: torch.Tensor | None, fmt: int, rows: int, cols: int,
+             name: str = "") -> None:
+    _packed(codes, name + "codes", torch.uint8, (rows, _code_bytes(fmt, cols)))
+    _packed(scales, name + "scales", torch.uint8, (rows, cols // QUEST_MX_GROUP))
+    _packed(mask, name + "mask", torch.uint8, (rows, cols // 8))
+
+
+def quest_hadamard_quantize_mx(x: torch.Tensor, had_block: int, fmt: int, *, codes: torch.Tensor, scales: torch.Tensor,
+                               mask: torch.Tensor | None = None) -> None:
+    """x [rows, cols] -> codes [rows, cols/2] (QUEST_MX_E2M1) or [rows, cols] (QUEST_MX_E4M3), a scale byte for each 32 elements
+    [rows, cols/32], trust bitmap [rows, cols/8] (uint8, caller-allocated)."""
+    rows, cols, ld = _rows(x, "x")
+    _operand(codes, scales, mask, fmt, rows, cols)
+    _check_devices(x, codes, scales, mask)
+    _check(load().quest_hadamard_quantize_mx(_ptr(x), _dtype_code(x), rows, cols, ld, had_block, fmt, _ptr(codes), _ptr(scales),
+                                             _ptr(mask), _stream()), "quest_hadamard_quantize_mx")
+
+
+def quest_dequantize_mx(codes: torch.Tensor, scales: torch.Tensor, fmt: int, *, out: torch.Tensor) -> None:
+    """out [rows, cols] (bf16 or fp32): what the codes and scales of quest_hadamard_quantize_mx stand for."""
+    rows, cols, ld = _rows(out, "out")
+    _operand(codes, scales, None, fmt, rows, cols)
+    _check_devices(codes, scales, out)
+    _check(load().quest_dequantize_mx(_ptr(codes), _ptr(scales), fmt, rows, cols, _ptr(out), _dtype_code(out), ld, _stream()),
+           "quest_dequantize_mx")
+
+
+def quest_lowbit_gemm_mx(a_codes: torch.Tensor, a_scales: torch.Tensor, a_format: int, b_codes: torch.Tensor,
+                         b_scales: torch.Tensor, K: int, *, y: torch.Tensor | None,
+                         acc_out: torch.Tensor | None = None) -> None:
+    """y[M, N] (bf16) and/or acc_out[M, N] (fp32) = a b^T: activations a in a_format, weights b in QUEST_MX_E2M1."""
+    M, N = a_codes.shape[0], b_codes.shape[0]
+    _operand(a_codes, a_scales, None, a_format, M, K, "a_")
+    _operand(b_codes, b_scales, None, QUEST_MX_E2M1, N, K, "b_")
+    ld_y = N
+    if y is not None:
+        if y.dtype != torch.bfloat16:
+            raise TypeError(f"unsupported tensor dtype {y.dtype}")
+        ld_y = _rows(y, "y", N, M)[2]
+    _packed(acc_out, "acc_out", torch.float32, (M, N))
+    _check_devices(a_codes, a_scales, b_codes, b_scales, y, acc_out)
+    _check(load().quest_lowbit_gemm_mx(_ptr(a_codes), _ptr(a_scales), a_format, M, _ptr(b_codes), _ptr(b_scales), N, K, _ptr(y),
+                                       ld_y, _ptr(acc_out), _stream()), "quest_lowbit_gemm_mx")
+
+
+def quest_grad_gemm_mx_workspace_bytes(which: int, M: int, N: int, K: int) -> int:
+    return int(load().quest_grad_gemm_mx_workspace_bytes(which, M, N, K))
+
+
+def quest_grad_gemm_mx(which: int, dy: torch.Tensor, q_codes: torch.Tensor, q_scales: torch.Tensor, q_format: int, M: int, N: int,
+                       K: int, *, out: torch.Tensor, workspace: torch.Tensor | None = None) -> None:
+    """quest_grad_gemm for a microscaled operand: weights [N, K] (which = 0) or activations [M, K] (which = 1)."""
+    _packed(dy, "dy", torch.bfloat16, (M, N))
+    _operand(q_codes, q_scales, None, q_format, M if which == 1 else N, K, "q_")
+    _packed(out, "out", torch.bfloat16, (N if which == 1 else M, K))
+    _check_devices(dy, q_codes, q_scales, out, workspace)
+    _check(load().quest_grad_gemm_mx(which, _ptr(dy), _ptr(q_codes), _ptr(q_scales), q_format, M, N, K, _ptr(out),
+                                     _ptr(workspace), _bytes(workspace), _stream()), "quest_grad_gemm_mx")
+
+
+def quest_rms_norm_mx(x: torch.Tensor, weight: torch.Tensor, eps: float, had_block: int = 1, fmt: int = QUEST_MX_E4M3, *,
+                      codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, mask: torch.Tensor | None = None,
+                      residual: torch.Tensor | None = None, h_out: torch.Tensor | None = None, y_out: torch.Tensor | None = None,
+                      rstd: torch.Tensor | None = None) -> None:
+    """h_out = x + residual; y_out = h * rstd * weight; codes, scales, mask: y as quest_hadamard_quantize_mx quantizes it."""
+    rows, cols, ld_x = _rows(x, "x")
+    ld_residual = _rows(residual, "residual", cols, rows)[2] if residual is not None else 0
+    if residual is not None and residual.dtype != x.dtype:
+        raise TypeError(f"residual is {residual.dtype}, x {x.dtype}")
+    _packed(weight, "weight", weight.dtype, (cols,))
+    _operand(codes, scales, mask, fmt, rows, cols)
+    _packed(h_out, "h_out", x.dtype, (rows, cols))
+    _packed(y_out, "y_out", x.dtype, (rows, cols))
+    _packed(rstd, "rstd", torch.float32, (rows,))
+    _check_devices(x, weight, codes, scales, mask, residual, h_out, y_out, rstd)
+    _check(load().quest_rms_norm_mx(_ptr(x), ld_x, _ptr(residual), ld_residual, _dtype_code(x), _ptr(weight), _dtype_code(weight),
+                                    rows, cols, eps, _ptr(h_out), _ptr(y_out), had_block, fmt, _ptr(codes), _ptr(scales),
+                                    _ptr(mask), _ptr(rstd), _stream()), "quest_rms_norm_mx")
+
+
+def quest_rms_norm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load().quest_rms_norm_backward_workspace_bytes(rows, cols))
+
+
+def quest_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, *, dx: torch.Tensor,
+                            dweight: torch.Tensor | None, dh: torch.Tensor | None = None,
+                            workspace: torch.Tensor | None = None) -> None:
+    """dx and dweight of quest_rms_norm_mx's y from dy, with dh added to dx (contiguous matrices of one dtype)."""
+    rows, cols, _ = _rows(h, "h")
+    for name, t in (("h", h), ("dy", dy), ("dh", dh), ("dx", dx)):
+        _packed(t, name, h.dtype, (rows, cols))
+    _packed(weight, "weight", weight.dtype, (cols,))
+    _packed(rstd, "rstd", torch.float32, (rows,))
+    _packed(dweight, "dweight", torch.float32, (cols,))
+    _check_devices(dy, h, weight, rstd, dh, dx, dweight, workspace)
+    _check(load().quest_rms_norm_backward(_ptr(dy), _ptr(h), _dtype_code(h), _ptr(weight), _dtype_code(weight), _ptr(rstd),
+                                          _ptr(dh), rows, cols, _ptr(dx), _ptr(dweight), _ptr(workspace), _bytes(workspace),
+                                          _stream()), "quest_rms_norm_backward")

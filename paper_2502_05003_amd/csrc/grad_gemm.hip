@@ -10,7 +10,7 @@
 #include <numeric>
 #include <utility>
 
-#include "gemm_tile.h"
+#include "mx_formats.h"
 #include "quest_internal.h"
 
 namespace quest {
@@ -151,6 +151,29 @@ __global__ __launch_bounds__(256) void expand_fp4_codes_kernel(const uint8_t *__
             out[decltype(pair)::value] = pack_bf16(__fmul_rn(s, u[0]), __fmul_rn(s, u[1]));
         });
         *reinterpret_cast<uint4 *>(qhat + (size_t)g * 8) = make_uint4(out[0], out[1], out[2], out[3]);
+    }
+}
+
+// Microscaled operands to bf16 (exact but at the ends of the range): four groups of eight codes per thread
+template <int FORMAT>
+__global__ __launch_bounds__(256) void expand_mx_codes_kernel(const uint8_t *__restrict__ codes,
+                                                              const uint8_t *__restrict__ scales, uint32_t groups,
+                                                              uint16_t *__restrict__ qhat)
+{
+    constexpr int kWords = MxFormat<FORMAT>::kWords;
+#pragma unroll
+    for (int part = 0; part < 4; ++part) {
+        const uint32_t g = blockIdx.x * 1024u + part * 256u + threadIdx.x;   // group of eight elements
+        if (g >= groups)
+            continue;
+        uint32_t words[kWords];
+#pragma unroll
+        for (int w = 0; w < kWords; ++w)
+            words[w] = reinterpret_cast<const uint32_t *>(codes)[(size_t)g * kWords + w];
+        float v[8];
+        mx_decode<FORMAT>(words, scales[g / 4], v);
+        *reinterpret_cast<uint4 *>(qhat + (size_t)g * 8) =
+            make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
     }
 }
 
@@ -857,7 +880,7 @@ hipError_t launch_grad_gemm(const GradGemmArgs &a, hipStream_t stream)
     const GradGemmPlan p = plan_grad_gemm(a.which, a.fp4 ? 0 : a.bits, a.M, a.N, a.K, device_compute_units());
     if (!p.covered)
         return hipErrorInvalidValue;
-    if (p.mid) {
+    if (p.mid && a.mx_scales == nullptr) {
         const GradMidArgs mid = {a.which, a.fp4 ? 0 : a.bits, a.dy, p.ld_left, a.q_codes, a.K * a.cb / 8, a.q_scales,
                                  p.contraction, p.out_rows, p.out_cols, a.out};
         return launch_grad_gemm_mid(mid, stream);
@@ -873,7 +896,12 @@ hipError_t launch_grad_gemm(const GradGemmArgs &a, hipStream_t stream)
     auto *partial = p.split ? reinterpret_cast<float4 *>(memory + p.expanded_bytes) : nullptr;
 
     const int64_t groups = p.q_rows * a.K / 8;
-    if (a.fp4)   // (the tile path's operands are below 2^30 elements: 32-bit group numbers)
+    if (a.mx_scales)
+        hipLaunchKernelGGL(a.mx_format == QUEST_MX_E4M3 ? expand_mx_codes_kernel<QUEST_MX_E4M3>
+                                                        : expand_mx_codes_kernel<QUEST_MX_E2M1>,
+                           dim3((unsigned)((groups + 1023) / 1024)), dim3(256), 0, stream, a.q_codes, a.mx_scales,
+                           (uint32_t)groups, qhat);
+    else if (a.fp4)   // (the tile path's operands are below 2^30 elements: 32-bit group numbers)
         hipLaunchKernelGGL(expand_fp4_codes_kernel, dim3((unsigned)((groups + 511) / 512)), dim3(256), 0, stream,
                            a.q_codes, a.q_scales, (uint32_t)(a.K / 8), (uint32_t)groups, qhat);
     else

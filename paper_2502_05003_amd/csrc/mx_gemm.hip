@@ -1,0 +1,173 @@
+// y = a b^T on microscaled operands: activations in E2M1 or E4M3, weights in E2M1, a power-of-two scale for each 32 elements of
+// a row, which the matrix instruction (v_mfma_scale_f32_16x16x128_f8f6f4) applies itself.
+//
+// Operands of the instruction, K = 128: lane l holds row l % 16 of its operand and the scale byte of the elements 32 q .. + 32,
+// q = l / 16.  E2M1: those 32 elements, 16 bytes.  E4M3: elements 16 q .. + 16 and 64 + 16 q .. + 16, 16 bytes each.
+#include "mx_formats.h"
+#include "quest_internal.h"
+
+namespace quest {
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+constexpr int kUnit = 128;
+constexpr int kF4 = 4, kF8 = 0;   // the instruction's codes for E2M1 and E4M3
+
+template <int FORMAT>
+struct MxOperand {
+    static constexpr bool kE4M3 = FORMAT == QUEST_MX_E4M3;
+    static constexpr int kUnitBytes = kE4M3 ? 128 : 64;   // of a row
+    uint4 lo, hi;
+    uint32_t scale;
+
+    __device__ __forceinline__ void load(const uint8_t *codes, const uint8_t *scales, int unit, int quarter)
+    {
+        const uint8_t *p = codes + unit * kUnitBytes + 16 * quarter;
+        lo = *reinterpret_cast<const uint4 *>(p);
+        if constexpr (kE4M3)
+            hi = *reinterpret_cast<const uint4 *>(p + 64);
+        scale = *reinterpret_cast<const uint32_t *>(scales + 4 * unit) >> (8 * quarter);
+    }
+    __device__ __forceinline__ v8i operand() const
+    {
+        if constexpr (kE4M3)
+            return v8i{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+        else
+            return v8i{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, 0, 0, 0, 0};
+    }
+};
+
+// blockIdx.x: weight rows 16 NT blockIdx.x .., blockIdx.y: activation rows 16 MT blockIdx.y ..; the waves share the contraction
+// in units of 128 and meet in LDS.  The weights are the row operand, so a lane's four sums are consecutive outputs of a row.
+template <int FORMAT, int MT, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void mx_few_kernel(const uint8_t *__restrict__ a_codes,
+                                                            const uint8_t *__restrict__ a_scales,
+                                                            const uint8_t *__restrict__ b_codes,
+                                                            const uint8_t *__restrict__ b_scales, int M, int N, int K,
+                                                            uint16_t *__restrict__ y, int64_t ld_y, float *__restrict__ acc_out)
+{
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    typedef MxOperand<FORMAT> A;
+    typedef MxOperand<QUEST_MX_E2M1> B;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int row16 = lane & 15, quarter = lane >> 4;
+    const int n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16 * MT;
+    const int units = K / kUnit;
+
+    const uint8_t *a_row[MT], *b_row[NT], *a_scale[MT], *b_scale[NT];   // rows beyond the edge read the last row, not stored
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t row = min(m0 + 16 * i + row16, M - 1);
+        a_row[i] = a_codes + row * units * A::kUnitBytes;
+        a_scale[i] = a_scales + row * units * 4;
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int64_t row = min(n0 + 16 * j + row16, N - 1);
+        b_row[j] = b_codes + row * units * B::kUnitBytes;
+        b_scale[j] = b_scales + row * units * 4;
+    }
+    v4f acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            acc[i][j] = v4f{0, 0, 0, 0};
+    for (int u = wave; u < units; u += WAVES) {
+        A a[MT];
+        B b[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            b[j].load(b_row[j], b_scale[j], u, quarter);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            a[i].load(a_row[i], a_scale[i], u, quarter);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j].operand(), a[i].operand(), acc[i][j], kF4,
+                                                                             A::kE4M3 ? kF8 : kF4, 0, (int)b[j].scale, 0,
+                                                                             (int)a[i].scale);
+    }
+    // the waves' sums, added in their order: [wave][i][j][lane]
+    v4f *park = reinterpret_cast<v4f *>(smem);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            park[((wave * MT + i) * NT + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    const bool quad_ok = (ld_y & 3) == 0 && (reinterpret_cast<uintptr_t>(y) & 7) == 0;
+    for (int t = tid; t < MT * NT * 64; t += 64 * WAVES) {
+        v4f sum = park[t];
+#pragma unroll
+        for (int v = 1; v < WAVES; ++v)
+            sum += park[v * (MT * NT * 64) + t];
+        const int tile = t >> 6, l = t & 63;
+        const int m = m0 + 16 * (tile / NT) + (l & 15), n = n0 + 16 * (tile % NT) + 4 * (l >> 4);
+        if (m >= M || n >= N)
+            continue;
+        if (acc_out) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < N)
+                    acc_out[(int64_t)m * N + n + e] = sum[e];
+        }
+        if (!y)
+            continue;
+        uint16_t *dst = y + (int64_t)m * ld_y + n;
+        if (quad_ok && n + 4 <= N) {
+            *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < N)
+                    dst[e] = (uint16_t)float_to_bf16_bits(sum[e]);
+        }
+    }
+}
+
+template <int FORMAT, int MT, int NT, int WAVES>
+hipError_t launch_few(const MxGemmArgs &a, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((a.N + 16 * NT - 1) / (16 * NT)), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
+    hipLaunchKernelGGL((mx_few_kernel<FORMAT, MT, NT, WAVES>), grid, dim3(64 * WAVES), WAVES * MT * NT * 1024, stream, a.a_codes,
+                       a.a_scales, a.b_codes, a.b_scales, (int)a.M, (int)a.N, (int)a.K, static_cast<uint16_t *>(a.y), a.ld_y,
+                       a.acc_out);
+    return hipGetLastError();
+}
+
+template <int FORMAT>
+hipError_t launch_format(const MxGemmArgs &a, hipStream_t stream)
+{
+    return a.M <= 16 ? launch_few<FORMAT, 1, 1, 8>(a, stream) : launch_few<FORMAT, 4, 4, 4>(a, stream);
+}
+
+}  // namespace
+
+hipError_t prepare_mx_gemm_kernels()
+{
+    static OncePerDevice once;
+    return once([] {
+        hipError_t err = allow_dynamic_lds(reinterpret_cast<const void *>(mx_few_kernel<QUEST_MX_E2M1, 4, 4, 4>), 64 << 10);
+        if (err == hipSuccess)
+            err = allow_dynamic_lds(reinterpret_cast<const void *>(mx_few_kernel<QUEST_MX_E4M3, 4, 4, 4>), 64 << 10);
+        return err;
+    });
+}
+
+hipError_t launch_mx_gemm(const MxGemmArgs &a, hipStream_t stream)
+{
+    if (a.M == 0 || a.N == 0)
+        return hipSuccess;
+    const hipError_t err = prepare_mx_gemm_kernels();
+    if (err != hipSuccess)
+        return err;
+    return a.a_format == QUEST_MX_E4M3 ? launch_format<QUEST_MX_E4M3>(a, stream) : launch_format<QUEST_MX_E2M1>(a, stream);
+}
+
+}  // namespace quest

@@ -624,6 +624,197 @@ quest_status quest_weight_only_gemm(const void *x, const uint8_t *w_codes, const
                              stream);
 }
 
+namespace {
+
+// Arguments that a microscaled operand's producers share
+quest_status mx_shape_checks(int64_t rows, int64_t cols, int64_t had_block, int64_t largest_block, int *log2n)
+{
+    if (rows < 0 || cols < QUEST_MX_GROUP || cols > QUEST_MAX_COLS || (cols % QUEST_MX_GROUP) || rows > QUEST_MAX_MX_ROWS ||
+        rows * cols > (int64_t(1) << 34))   // (a launch has fewer than 2^32 threads: eight elements each, or 256 for a row)
+        return QUEST_ERR_SHAPE;
+    const int l = exact_log2(had_block);
+    if (l < 0 || had_block > largest_block || cols % had_block)
+        return QUEST_ERR_BLOCK;
+    *log2n = l;
+    return QUEST_OK;
+}
+
+bool known_dtype(quest_dtype dtype)
+{
+    return dtype == QUEST_F32 || dtype == QUEST_BF16;
+}
+
+bool known_format(quest_mx_format format)
+{
+    return format == QUEST_MX_E2M1 || format == QUEST_MX_E4M3;
+}
+
+int64_t bytes_of(quest_dtype dtype)
+{
+    return dtype == QUEST_BF16 ? 2 : 4;
+}
+
+quest_status launched(hipError_t err)
+{
+    return err == hipSuccess ? QUEST_OK : QUEST_ERR_LAUNCH;
+}
+
+}  // namespace
+
+quest_status quest_hadamard_quantize_mx(const void *x, quest_dtype dtype, int64_t rows, int64_t cols, int64_t ld,
+                                        int32_t had_block, quest_mx_format format, uint8_t *codes, uint8_t *scales,
+                                        uint8_t *mask, void *stream)
+{
+    if (rows != 0 && (!x || !codes || !scales))
+        return QUEST_ERR_NULL;
+    if (!known_dtype(dtype) || !known_format(format))
+        return QUEST_ERR_DTYPE;
+    int log2n = 0;
+    const quest_status shape = mx_shape_checks(rows, cols, had_block, QUEST_MAX_HAD_BLOCK, &log2n);
+    if (shape != QUEST_OK)
+        return shape;
+    if (ld < cols)
+        return QUEST_ERR_SHAPE;
+    if (!aligned16(x) || !aligned16(codes) || !aligned16(mask) || ((ld * bytes_of(dtype)) & 15))
+        return QUEST_ERR_ALIGN;
+    const quest::MxQuantizeArgs args = {x, dtype, rows, cols, ld, log2n, format, codes, scales, mask};
+    return launched(quest::launch_mx_quantize(args, static_cast<hipStream_t>(stream)));
+}
+
+quest_status quest_dequantize_mx(const uint8_t *codes, const uint8_t *scales, quest_mx_format format, int64_t rows,
+                                 int64_t cols, void *out, quest_dtype out_dtype, int64_t ld, void *stream)
+{
+    if (rows != 0 && (!codes || !scales || !out))
+        return QUEST_ERR_NULL;
+    if (!known_dtype(out_dtype) || !known_format(format))
+        return QUEST_ERR_DTYPE;
+    int log2n = 0;
+    const quest_status shape = mx_shape_checks(rows, cols, 1, 1, &log2n);
+    if (shape != QUEST_OK)
+        return shape;
+    if (ld < cols)
+        return QUEST_ERR_SHAPE;
+    if (!aligned16(codes) || !aligned16(out) || ((ld * bytes_of(out_dtype)) & 15))
+        return QUEST_ERR_ALIGN;
+    const quest::MxDequantizeArgs args = {codes, scales, format, rows, cols, out, out_dtype, ld};
+    return launched(quest::launch_mx_dequantize(args, static_cast<hipStream_t>(stream)));
+}
+
+quest_status quest_lowbit_gemm_mx(const uint8_t *a_codes, const uint8_t *a_scales, quest_mx_format a_format, int64_t M,
+                                  const uint8_t *b_codes, const uint8_t *b_scales, int64_t N, int64_t K, void *y,
+                                  int64_t ld_y, float *acc_out, void *stream)
+{
+    const int64_t limit = int64_t(1) << 22;
+    if (M != 0 && N != 0 && (!a_codes || !a_scales || !b_codes || !b_scales || (!y && !acc_out)))
+        return QUEST_ERR_NULL;
+    if (!known_format(a_format))
+        return QUEST_ERR_DTYPE;
+    if (M < 0 || N < 0 || M > limit || N > limit || K < 128 || K > 65536 || (K & 127) || (y && ld_y < N))
+        return QUEST_ERR_SHAPE;
+    if (!aligned16(a_codes) || !aligned16(b_codes) || (reinterpret_cast<uintptr_t>(a_scales) & 3u) ||
+        (reinterpret_cast<uintptr_t>(b_scales) & 3u) || (reinterpret_cast<uintptr_t>(y) & 1u) ||
+        (reinterpret_cast<uintptr_t>(acc_out) & 3u))
+        return QUEST_ERR_ALIGN;
+    const quest::MxGemmArgs args = {a_codes, a_scales, a_format, b_codes, b_scales, M, N, K, y, ld_y, acc_out};
+    return launched(quest::launch_mx_gemm(args, static_cast<hipStream_t>(stream)));
+}
+
+int64_t quest_grad_gemm_mx_workspace_bytes(int32_t which, int64_t M, int64_t N, int64_t K)
+{
+    return quest_grad_gemm_fp4_workspace_bytes(which, M, N, K);   // the expanded operand is the same
+}
+
+quest_status quest_grad_gemm_mx(int32_t which, const void *dy, const uint8_t *q_codes, const uint8_t *q_scales,
+                                quest_mx_format q_format, int64_t M, int64_t N, int64_t K, void *out, void *workspace,
+                                int64_t workspace_bytes, void *stream)
+{
+    if (which != 0 && which != 1)
+        return QUEST_ERR_ARG;
+    if (!dy || !q_codes || !q_scales || !out)
+        return QUEST_ERR_NULL;
+    if (!known_format(q_format))
+        return QUEST_ERR_DTYPE;
+    const int64_t needed = quest_grad_gemm_mx_workspace_bytes(which, M, N, K);
+    if (needed < 0)
+        return QUEST_ERR_SHAPE;
+    if (!aligned16(dy) || !aligned16(q_codes) || !aligned16(out) || !aligned16(workspace))
+        return QUEST_ERR_ALIGN;
+    if (workspace_bytes < 0 || (needed > 0 && (!workspace || workspace_bytes < needed)))
+        return QUEST_ERR_ARG;
+
+    quest::GradGemmArgs args;
+    args.which = which;
+    args.fp4 = true;
+    args.dy = dy;
+    args.q_codes = q_codes;
+    args.q_scales = nullptr;
+    args.bits = 4;
+    args.cb = q_format == QUEST_MX_E4M3 ? 8 : 4;
+    args.M = M;
+    args.N = N;
+    args.K = K;
+    args.out = out;
+    args.workspace = workspace;
+    args.workspace_bytes = workspace_bytes;
+    args.mx_scales = q_scales;
+    args.mx_format = q_format;
+    return launched(quest::launch_grad_gemm(args, static_cast<hipStream_t>(stream)));
+}
+
+quest_status quest_rms_norm_mx(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual, quest_dtype dtype,
+                               const void *weight, quest_dtype weight_dtype, int64_t rows, int64_t cols, float eps,
+                               void *h_out, void *y_out, int32_t had_block, quest_mx_format format, uint8_t *codes,
+                               uint8_t *scales, uint8_t *mask, float *rstd, void *stream)
+{
+    if (!weight || (rows != 0 && (!x || (codes == nullptr && y_out == nullptr))))
+        return QUEST_ERR_NULL;
+    if (!known_dtype(dtype) || !known_dtype(weight_dtype) || (codes && !known_format(format)))
+        return QUEST_ERR_DTYPE;
+    int log2n = 0;
+    const quest_status shape = mx_shape_checks(rows, cols, codes ? had_block : 1, QUEST_MAX_NORM_HAD_BLOCK, &log2n);
+    if (shape != QUEST_OK)
+        return shape;
+    if (ld_x < cols || (residual && ld_residual < cols))
+        return QUEST_ERR_SHAPE;
+    const int64_t elem = bytes_of(dtype);
+    if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(h_out) || !aligned16(y_out) ||
+        !aligned16(codes) || !aligned16(mask) || ((ld_x * elem) & 15) || (residual && ((ld_residual * elem) & 15)) ||
+        (reinterpret_cast<uintptr_t>(rstd) & 3u))
+        return QUEST_ERR_ALIGN;
+    if (!(eps >= 0.0f) || isinf(eps) || (residual == nullptr) != (h_out == nullptr) ||
+        (codes == nullptr) != (scales == nullptr) || (mask && !codes))
+        return QUEST_ERR_ARG;
+    const quest::RmsNormArgs args = {x, ld_x, residual, ld_residual, dtype, weight, weight_dtype, rows, cols, eps,
+                                     h_out, y_out, log2n, format, codes, scales, mask, rstd};
+    return launched(quest::launch_rms_norm(args, static_cast<hipStream_t>(stream)));
+}
+
+int64_t quest_rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols)
+{
+    int log2n = 0;
+    return mx_shape_checks(rows, cols, 1, 1, &log2n) == QUEST_OK ? quest::rms_norm_backward_workspace_bytes(rows, cols) : -1;
+}
+
+quest_status quest_rms_norm_backward(const void *dy, const void *h, quest_dtype dtype, const void *weight,
+                                     quest_dtype weight_dtype, const float *rstd, const void *dh, int64_t rows, int64_t cols,
+                                     void *dx, float *dweight, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (!weight || (rows != 0 && (!dy || !h || !rstd || !dx)))
+        return QUEST_ERR_NULL;
+    if (!known_dtype(dtype) || !known_dtype(weight_dtype))
+        return QUEST_ERR_DTYPE;
+    const int64_t needed = quest_rms_norm_backward_workspace_bytes(rows, cols);
+    if (needed < 0)
+        return QUEST_ERR_SHAPE;
+    if (!aligned16(dy) || !aligned16(h) || !aligned16(weight) || !aligned16(dh) || !aligned16(dx) || !aligned16(dweight) ||
+        !aligned16(workspace) || (reinterpret_cast<uintptr_t>(rstd) & 3u))
+        return QUEST_ERR_ALIGN;
+    if (workspace_bytes < 0 || (dweight && needed > 0 && (!workspace || workspace_bytes < needed)))
+        return QUEST_ERR_ARG;
+    const quest::RmsNormBackwardArgs args = {dy, h, dtype, weight, weight_dtype, rstd, dh, rows, cols, dx, dweight, workspace};
+    return launched(quest::launch_rms_norm_backward(args, static_cast<hipStream_t>(stream)));
+}
+
 quest_plan quest_plan_forward(int32_t bits, int64_t M, int64_t N, int64_t K, int32_t with_workspace)
 {
     return bits == 0 ? quest::plan_fp4_gemm(M, N, K) : quest::plan_lowbit_gemm(M, N, K, bits, with_workspace != 0);
@@ -654,6 +845,12 @@ quest_status quest_init(void)
             err = quest::prepare_grad_gemm_kernels();
         if (err == hipSuccess)
             err = quest::prepare_grad_gemm_mid_kernels();
+        if (err == hipSuccess)
+            err = quest::prepare_mx_quantize_kernels();
+        if (err == hipSuccess)
+            err = quest::prepare_mx_gemm_kernels();
+        if (err == hipSuccess)
+            err = quest::prepare_rms_norm_kernels();
         void *ptr = nullptr;
         if (err == hipSuccess)
             err = static_scratch_address(&ptr);

@@ -97,6 +97,72 @@ struct SkinnyGemmArgs {
 bool skinny_gemm_preferred(int64_t M, int64_t N, int64_t K, int grid);
 hipError_t launch_skinny_gemm(const SkinnyGemmArgs &a, hipStream_t stream);
 
+// Microscaled operands (csrc/mx_formats.h)
+struct MxQuantizeArgs {
+    const void *x;
+    quest_dtype dtype;
+    int64_t rows, cols, ld;
+    int log2n;
+    quest_mx_format format;
+    uint8_t *codes, *scales;
+    uint8_t *mask;     // may be null
+};
+hipError_t launch_mx_quantize(const MxQuantizeArgs &a, hipStream_t stream);
+
+struct MxDequantizeArgs {
+    const uint8_t *codes, *scales;
+    quest_mx_format format;
+    int64_t rows, cols;
+    void *out;
+    quest_dtype out_dtype;
+    int64_t ld;
+};
+hipError_t launch_mx_dequantize(const MxDequantizeArgs &a, hipStream_t stream);
+
+struct MxGemmArgs {
+    const uint8_t *a_codes, *a_scales;
+    quest_mx_format a_format;
+    const uint8_t *b_codes, *b_scales;   // E2M1
+    int64_t M, N, K;
+    void *y;          // bf16, may be null
+    int64_t ld_y;
+    float *acc_out;   // may be null
+};
+hipError_t launch_mx_gemm(const MxGemmArgs &a, hipStream_t stream);
+
+struct RmsNormArgs {
+    const void *x;
+    int64_t ld_x;
+    const void *residual;   // may be null, like h_out then
+    int64_t ld_residual;
+    quest_dtype dtype;
+    const void *weight;
+    quest_dtype weight_dtype;
+    int64_t rows, cols;
+    float eps;
+    void *h_out, *y_out;    // y_out may be null
+    int log2n;
+    quest_mx_format format;
+    uint8_t *codes, *scales, *mask;   // may be null: y_out alone
+    float *rstd;            // may be null
+};
+hipError_t launch_rms_norm(const RmsNormArgs &a, hipStream_t stream);
+
+struct RmsNormBackwardArgs {
+    const void *dy, *h;
+    quest_dtype dtype;
+    const void *weight;
+    quest_dtype weight_dtype;
+    const float *rstd;
+    const void *dh;         // may be null
+    int64_t rows, cols;
+    void *dx;
+    float *dweight;         // may be null; the workspace holds the partial sums for it
+    void *workspace;
+};
+hipError_t launch_rms_norm_backward(const RmsNormBackwardArgs &a, hipStream_t stream);
+int64_t rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+
 struct BackwardArgs {
     const void *g;
     quest_dtype g_dtype;
@@ -132,6 +198,9 @@ struct GradGemmArgs {
     void *out;
     void *workspace;   // caller's scratch: the expanded operand, then the partial tiles
     int64_t workspace_bytes;
+    // a microscaled operand: its scales in place of q_scales, and its format
+    const uint8_t *mx_scales = nullptr;
+    quest_mx_format mx_format = QUEST_MX_E2M1;
 };
 
 // The same products for outputs of few tiles (grad_gemm_mid.hip); needs no scratch.
@@ -179,6 +248,9 @@ hipError_t prepare_fp4_gemm_kernels();
 hipError_t prepare_trust_backward_kernels();
 hipError_t prepare_grad_gemm_kernels();
 hipError_t prepare_grad_gemm_mid_kernels();
+hipError_t prepare_mx_quantize_kernels();
+hipError_t prepare_mx_gemm_kernels();
+hipError_t prepare_rms_norm_kernels();
 
 // Runs a set-up step until it has succeeded once on the current device; afterwards the cost is the question
 // which device that is (a call's path through the locks and look-ups of six limits was 0.5 us).  Safe

@@ -1,0 +1,516 @@
+"""Microscaled operands on the GPU: quantizer, what codes stand for, product, gradients, and the norm in front, against the
+64-bit definitions of oracle/microscaled.py."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import microscaled as mx
+from oracle import quest_oracle as qo
+from paper_2502_05003_amd import binding as q
+
+from gpu_util import DEV, bf16_bits, to_host_f64
+
+pytestmark = pytest.mark.gpu
+
+E2M1, E4M3 = q.QUEST_MX_E2M1, q.QUEST_MX_E4M3
+BF16, F32 = torch.bfloat16, torch.float32
+HALF = {BF16: 2.0 ** -8, F32: 2.0 ** -24}      # largest relative error of one rounding
+
+
+def rows_of(rows, cols, dtype, seed, std=1.0):
+    """Gaussian rows with outlier columns and rows of very different size."""
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((rows, cols)) * std * np.exp(rng.uniform(-3, 3, size=(rows, 1)))
+    x[:, rng.permutation(cols)[:max(1, cols // 100)]] *= 30
+    return torch.from_numpy(x.astype(np.float32)).to(dtype)
+
+
+def buffers(rows, cols, fmt, mask=True):
+    out = dict(codes=torch.full((rows, cols if fmt == E4M3 else cols // 2), 0xAA, dtype=torch.uint8, device=DEV),
+               scales=torch.full((rows, cols // 32), 0x55, dtype=torch.uint8, device=DEV))
+    if mask:
+        out["mask"] = torch.full((rows, cols // 8), 0x33, dtype=torch.uint8, device=DEV)
+    return out
+
+
+def host(t):
+    return t.cpu().numpy()
+
+
+def random_operand(rows, cols, fmt, seed, low=110, high=140):
+    """Every code value (E4M3: no NaN), scales over a range of exponents."""
+    rng = np.random.default_rng(seed)
+    codes = rng.integers(0, 256, size=(rows, cols if fmt == E4M3 else cols // 2), dtype=np.uint8)
+    if fmt == E4M3:
+        codes[(codes & 127) == 127] = 0x38
+    scales = rng.integers(low, high, size=(rows, cols // 32), dtype=np.uint8)
+    return codes, scales
+
+
+def on_device(*arrays):
+    return [torch.from_numpy(np.ascontiguousarray(a)).to(DEV) for a in arrays]
+
+
+# ---- quantizer
+
+def check_quantized(x, block, fmt, got):
+    """Bit for bit: the transform's order of additions is fixed, the rest is exact."""
+    xh = mx.hadamard_f32(x.float().numpy(), block)
+    with np.errstate(invalid="ignore"):
+        code, scales, trust = mx.quantize(xh, fmt)
+    assert np.array_equal(host(got["scales"]), scales)
+    assert np.array_equal(host(got["codes"]), mx.pack(code, fmt))
+    if "mask" in got:
+        assert np.array_equal(host(got["mask"]), mx.pack_mask(trust))
+    return xh
+
+
+SHAPES = [(1, 32, 1), (1, 32, 32), (3, 96, 32), (3, 96, 16), (5, 640, 128), (777, 640, 2), (129, 512, 512), (64, 1280, 256),
+          (33, 5632, 1), (24, 5632, 512), (7, 2048, 1024), (2, 16384, 16384), (3, 5632, 8), (2, 2048, 4), (300, 4096, 64)]
+
+
+@pytest.mark.parametrize("rows,cols,block", SHAPES)
+@pytest.mark.parametrize("fmt", [E2M1, E4M3])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_quantizer(rows, cols, block, fmt, dtype):
+    x = rows_of(rows, cols, dtype, rows + cols + block)
+    got = buffers(rows, cols, fmt)
+    q.quest_hadamard_quantize_mx(x.to(DEV), block, fmt, **got)
+    xh = check_quantized(x, block, fmt, got)
+    exact = qo.hadamard(x.double().numpy(), block)
+    assert np.all(np.abs(xh - exact) <= 1e-5 * np.maximum(np.abs(exact), np.sqrt((exact ** 2).mean(-1, keepdims=True))))
+
+
+@pytest.mark.parametrize("block,ld", [(32, 176), (16, 168), (1024, 2056)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_quantizer_strided_rows_without_a_mask(block, ld, dtype):
+    cols = 160 if block < 160 else 2048
+    x = rows_of(37, ld, dtype, 3)[:, :cols]
+    got = buffers(37, cols, E2M1, mask=False)
+    q.quest_hadamard_quantize_mx(x.to(DEV)[:, :], block, E2M1, **got)
+    wide = rows_of(37, ld, dtype, 3).to(DEV)
+    again = buffers(37, cols, E2M1, mask=False)
+    q.quest_hadamard_quantize_mx(wide[:, :cols], block, E2M1, **again)
+    check_quantized(x, block, E2M1, again)
+    assert torch.equal(got["codes"], again["codes"]) and torch.equal(got["scales"], again["scales"])
+
+
+@pytest.mark.parametrize("fmt", [E2M1, E4M3])
+def test_quantizer_borders(fmt):
+    """Ties, the clip and trust borders, zeros of both signs, subnormal and huge groups, infinities and NaN, each group alone."""
+    grid = mx.MAGNITUDES[fmt]
+    mids = (grid[1:] + grid[:-1]) / 2
+    largest, trusted = grid[-1], mx.TRUSTED[fmt]
+    points = np.concatenate([grid, mids, np.nextafter(mids.astype(np.float32), np.float32(0)),
+                             np.nextafter(mids.astype(np.float32), np.float32(1e9)),
+                             [trusted, np.nextafter(np.float32(trusted), np.float32(1e9)), largest * 8 / 7 * 0.999]])
+    groups = []
+    for at in range(0, len(points), 15):
+        g = np.zeros(32, dtype=np.float32)
+        g[0] = largest                                # fixes the scale at 1
+        part = points[at:at + 15]
+        g[1:1 + len(part)], g[17:17 + len(part)] = part, -part
+        groups.append(g)
+    groups.append(np.zeros(32, dtype=np.float32))
+    groups.append(-np.zeros(32, dtype=np.float32))
+    for scale in (2.0 ** -149, 2.0 ** -126, 2.0 ** -120, 2.0 ** 100, 2.0 ** 119):
+        groups.append((groups[0] * np.float32(scale)).astype(np.float32))
+    groups.append(np.full(32, np.finfo(np.float32).max, dtype=np.float32))
+    for bad in (np.inf, -np.inf, np.nan):
+        g = groups[0].copy()
+        g[13] = bad
+        groups += [g, groups[1].copy()]               # the group behind is not affected
+    x = torch.from_numpy(np.stack(groups).reshape(1, -1))
+    got = buffers(1, x.shape[1], fmt)
+    q.quest_hadamard_quantize_mx(x.to(DEV), 1, fmt, **got)
+    check_quantized(x, 1, fmt, got)
+
+
+def test_quantizer_leaves_what_is_behind_its_outputs():
+    x = rows_of(5, 96, BF16, 1).to(DEV)
+    codes, scales, mask = (torch.full((4096,), 0x77, dtype=torch.uint8, device=DEV) for _ in range(3))
+    q.quest_hadamard_quantize_mx(x, 32, E2M1, codes=codes[:240].view(5, 48), scales=scales[:15].view(5, 3),
+                                 mask=mask[:60].view(5, 12))
+    assert bool((codes[240:] == 0x77).all() and (scales[15:] == 0x77).all() and (mask[60:] == 0x77).all())
+
+
+def test_scales_at_any_alignment():
+    x = rows_of(5, 96, BF16, 1)
+    spare = torch.zeros(64, dtype=torch.uint8, device=DEV)
+    for offset in (1, 2, 3):
+        got = buffers(5, 96, E4M3)
+        got["scales"] = spare[offset:offset + 15].view(5, 3)
+        q.quest_hadamard_quantize_mx(x.to(DEV), 32, E4M3, **got)
+        check_quantized(x, 32, E4M3, got)
+
+
+@pytest.mark.parametrize("fmt", [E2M1, E4M3])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_what_codes_stand_for(fmt, dtype):
+    """Every code with every scale: exact, or one rounding where bf16 has no such value; NaN and infinities where they belong."""
+    count = 256 if fmt == E4M3 else 32
+    codes = np.arange(256, dtype=np.uint8)[None, :].repeat(256, 0) if fmt == E4M3 else \
+        mx.pack(np.arange(32, dtype=np.uint8)[None, :].repeat(256, 0) & 15, E2M1)
+    scales = np.arange(256, dtype=np.uint8)[:, None].repeat(count // 32, 1)
+    out = torch.empty(256, count, dtype=dtype, device=DEV)
+    q.quest_dequantize_mx(*on_device(codes, scales), fmt, out=out)
+    with np.errstate(over="ignore"):
+        expected = torch.from_numpy(mx.values(codes, scales, fmt).astype(np.float32)).to(dtype)
+    got = out.cpu()
+    assert torch.equal(got.isnan(), expected.isnan())
+    assert torch.equal(got.nan_to_num(0.0, posinf=torch.inf, neginf=-torch.inf),
+                       expected.nan_to_num(0.0, posinf=torch.inf, neginf=-torch.inf))
+
+
+def test_what_codes_stand_for_strided_and_ragged():
+    codes, scales = random_operand(77, 96, E2M1, 5)
+    wide = torch.full((77, 112), -3.0, device=DEV)
+    q.quest_dequantize_mx(*on_device(codes, scales), E2M1, out=wide[:, :96])
+    assert np.array_equal(host(wide[:, :96]).astype(np.float64), mx.values(codes, scales, E2M1))
+    assert bool((wide[:, 96:] == -3.0).all())
+
+
+# ---- product
+
+def product_bound(a, b, fmt):
+    """Per output: fp32 accumulation (each of K products and their sums rounds by 2^-24 of what has been added up; the waves'
+    and stages' partial sums stay within that), and with E4M3 what the matrix instruction drops: of each product at most 2^-13
+    of the largest in its group of 32."""
+    K = a.shape[1]
+    bound = K * 2.0 ** -24 * (np.abs(a) @ np.abs(b).T)
+    if fmt == E4M3:
+        ga, gb = np.abs(a).reshape(len(a), K // 32, 32), np.abs(b).reshape(len(b), K // 32, 32)
+        for g in range(K // 32):
+            bound += 32 * 2.0 ** -13 * (ga[:, None, g] * gb[None, :, g]).max(-1)
+    return bound
+
+
+PRODUCTS = [(1, 1, 128), (1, 5632, 2048), (7, 33, 384), (16, 640, 5632), (24, 96, 1024), (65, 130, 256), (130, 257, 128),
+            (333, 512, 1024), (300, 1283, 640), (1030, 520, 512)]
+
+
+@pytest.mark.parametrize("M,N,K", PRODUCTS)
+@pytest.mark.parametrize("fmt", [E2M1, E4M3])
+def test_product(M, N, K, fmt):
+    (ac, as_), (bc, bs) = random_operand(M, K, fmt, M), random_operand(N, K, E2M1, N + 1)
+    a, b = mx.values(ac, as_, fmt), mx.values(bc, bs, E2M1)
+    y = torch.full((M, N), float("nan"), dtype=BF16, device=DEV)
+    acc = torch.full((M, N), float("nan"), device=DEV)
+    ac, as_, bc, bs = on_device(ac, as_, bc, bs)
+    q.quest_lowbit_gemm_mx(ac, as_, fmt, bc, bs, K, y=y, acc_out=acc)
+    ref, bound = a @ b.T, product_bound(a, b, fmt)
+    got = to_host_f64(acc)
+    assert np.all(np.abs(got - ref) <= bound + 2.0 ** -24 * np.abs(ref))
+    assert torch.equal(y, acc.to(BF16))
+    only = torch.empty_like(y)
+    q.quest_lowbit_gemm_mx(ac, as_, fmt, bc, bs, K, y=only)
+    assert torch.equal(only, y)
+    only_acc = torch.empty_like(acc)
+    q.quest_lowbit_gemm_mx(ac, as_, fmt, bc, bs, K, y=None, acc_out=only_acc)
+    assert torch.equal(only_acc, acc)
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 70, 256), (300, 322, 256)])
+@pytest.mark.parametrize("pitch", [0, 1, 2, 6, 8])
+def test_product_into_wider_rows(M, N, K, pitch):
+    """Rows of any pitch and start; what lies between them stays."""
+    (ac, as_), (bc, bs) = random_operand(M, K, E4M3, 1), random_operand(N, K, E2M1, 2)
+    ac, as_, bc, bs = on_device(ac, as_, bc, bs)
+    ref = torch.empty(M, N, dtype=BF16, device=DEV)
+    q.quest_lowbit_gemm_mx(ac, as_, E4M3, bc, bs, K, y=ref)
+    for start in (0, 1, 4):
+        flat = torch.full((start + M * (N + pitch) + 64,), -7.0, dtype=BF16, device=DEV)
+        y = flat[start:start + M * (N + pitch)].view(M, N + pitch)
+        q.quest_lowbit_gemm_mx(ac, as_, E4M3, bc, bs, K, y=y[:, :N])
+        assert torch.equal(y[:, :N], ref)
+        assert bool((y[:, N:] == -7.0).all()) and bool((flat[:start] == -7.0).all())
+        assert bool((flat[start + M * (N + pitch):] == -7.0).all())
+
+
+@pytest.mark.parametrize("M,N", [(3, 40), (260, 300)])
+@pytest.mark.parametrize("fmt", [E2M1, E4M3])
+def test_product_scales_at_their_ends(M, N, fmt):
+    """NaN groups reach their outputs and no others; large and small scales cancel."""
+    K = 256
+    ac, as_ = random_operand(M, K, fmt, 1, 1, 40)
+    bc, bs = random_operand(N, K, E2M1, 2, 214, 250)
+    as_[M // 2, 3] = 255
+    bs[N - 1, 7] = 255
+    a, b = mx.values(ac, as_, fmt), mx.values(bc, bs, E2M1)
+    acc = torch.empty(M, N, device=DEV)
+    q.quest_lowbit_gemm_mx(*on_device(ac, as_), fmt, *on_device(bc, bs), K, y=None, acc_out=acc)
+    with np.errstate(invalid="ignore"):
+        ref, bound = a @ b.T, product_bound(a, b, fmt)
+    got, nan = to_host_f64(acc), np.isnan(ref)
+    assert np.array_equal(np.isnan(got), nan) and nan[M // 2].all() and nan[:, N - 1].all() and nan.sum() == M + N - 1
+    assert np.all(np.abs(got - ref)[~nan] <= (bound + 2.0 ** -24 * np.abs(ref))[~nan])
+
+
+def test_empty_products():
+    for M, N in ((0, 5), (5, 0)):
+        (ac, as_), (bc, bs) = random_operand(M, 128, E2M1, 1), random_operand(N, 128, E2M1, 2)
+        q.quest_lowbit_gemm_mx(*on_device(ac, as_), E2M1, *on_device(bc, bs), 128, y=torch.empty(M, N, dtype=BF16, device=DEV))
+
+
+# ---- gradients
+
+def grad_scratch(which, M, N, K):
+    return torch.full((q.quest_grad_gemm_mx_workspace_bytes(which, M, N, K),), 0xC3, dtype=torch.uint8, device=DEV)
+
+
+@pytest.mark.parametrize("M,N,K", [(128, 128, 128), (192, 320, 448), (512, 128, 640), (2048, 448, 192), (128, 2048, 256)])
+@pytest.mark.parametrize("fmt", [E2M1, E4M3])
+@pytest.mark.parametrize("which", [0, 1])
+def test_gradient_products(M, N, K, fmt, which):
+    codes, scales = random_operand(M if which else N, K, fmt, K)
+    v = mx.values(codes, scales, fmt)
+    rng = np.random.default_rng(M)
+    dy = torch.from_numpy((0.03 * rng.standard_normal((M, N))).astype(np.float32)).to(BF16)
+    out = torch.full((N if which else M, K), float("nan"), dtype=BF16, device=DEV)
+    q.quest_grad_gemm_mx(which, dy.to(DEV), *on_device(codes, scales), fmt, M, N, K, out=out,
+                         workspace=grad_scratch(which, M, N, K))
+    d = dy.double().numpy()
+    left = d.T if which else d
+    ref = left @ v
+    # fp32 accumulation over the contraction, one rounding to bf16
+    bound = 2.0 ** -8 * np.abs(ref) + 2 * left.shape[1] * 2.0 ** -24 * (np.abs(left) @ np.abs(v))
+    assert np.all(np.abs(to_host_f64(out) - ref) <= bound)
+
+
+# ---- norm
+
+def norm_case(rows, cols, dtype, weight_dtype, seed):
+    rng = np.random.default_rng(seed)
+    x, r = rows_of(rows, cols, dtype, seed), rows_of(rows, cols, dtype, seed + 1, 2.0)
+    w = torch.from_numpy((1 + 0.2 * rng.standard_normal(cols)).astype(np.float32)).to(weight_dtype)
+    return x, r, w
+
+
+def rounded_to(a, dtype):
+    return torch.from_numpy(np.asarray(a)).to(dtype)
+
+
+NORMS = [(1, 32, 32), (3, 96, 1), (5, 640, 128), (24, 4096, 1), (7, 2048, 512), (2, 16384, 32), (130, 5632, 256), (9, 11008, 2)]
+
+
+@pytest.mark.parametrize("rows,cols,block", NORMS)
+@pytest.mark.parametrize("dtype,weight_dtype,fmt", [(BF16, F32, E4M3), (BF16, BF16, E2M1), (F32, F32, E2M1), (F32, BF16, E4M3)])
+@pytest.mark.parametrize("residual", [True, False])
+def test_norm(rows, cols, block, dtype, weight_dtype, fmt, residual):
+    x, r, w = norm_case(rows, cols, dtype, weight_dtype, rows + cols)
+    eps = 1e-5
+    h = (x.float() + r.float()).to(dtype) if residual else x
+    got = buffers(rows, cols, fmt)
+    h_out = torch.full((rows, cols), float("nan"), dtype=dtype, device=DEV) if residual else None
+    y = torch.full((rows, cols), float("nan"), dtype=dtype, device=DEV)
+    rstd = torch.full((rows,), float("nan"), device=DEV)
+    q.quest_rms_norm_mx(x.to(DEV), w.to(DEV), eps, block, fmt, residual=r.to(DEV) if residual else None, h_out=h_out, y_out=y,
+                        rstd=rstd, **got)
+    if residual:
+        assert torch.equal(h_out.cpu(), h)
+    y64, rstd64 = mx.rms_norm(h.double().numpy(), w.double().numpy(), eps)
+    # the sum of squares: cols additions at most, halved by the root; division, root and two products
+    off = (cols / 2 + 6) * 2.0 ** -24
+    assert np.all(np.abs(to_host_f64(rstd) - rstd64) <= off * rstd64)
+    assert np.all(np.abs(to_host_f64(y) - y64) <= (off + HALF[dtype] * (1 + off)) * np.abs(y64))
+    # the codes are those of the fp32 y: where fp32 is what y_out holds, bit for bit
+    if dtype == F32:
+        check_quantized(y.cpu(), block, fmt, got)
+    # a code stands for its element within half a step of the format's (the scale may fall to the other side of a power of two),
+    # clipped elements apart, which are those that are not trusted or lie beyond the largest element
+    xh = qo.hadamard(y64, block)
+    v = mx.values(host(got["codes"]), host(got["scales"]), fmt)
+    scale = np.repeat(np.ldexp(1.0, host(got["scales"]).astype(int) - 127), 32, axis=1)
+    half_step = scale * np.where(fmt == E2M1, 1.0, 16.0)       # of the widest interval
+    error = off * np.sqrt((np.abs(xh) ** 2).mean(-1, keepdims=True)) * np.sqrt(cols) + 1e-5 * np.abs(xh)
+    inside = np.abs(xh) <= mx.TRUSTED[fmt] * scale
+    assert np.all((np.abs(v - xh) <= half_step + error) | ~inside)
+    assert np.all(np.abs(v)[~inside] == mx.MAGNITUDES[fmt][-1] * scale[~inside])
+    trusted = np.unpackbits(host(got["mask"]), axis=1, bitorder="little").astype(bool)
+    near = np.abs(np.abs(xh) - mx.TRUSTED[fmt] * scale) <= error
+    assert np.all((trusted == inside) | near)
+
+
+def test_norm_outputs_alone():
+    """Without codes, without y, without rstd, from strided rows: the same numbers."""
+    x, r, w = (t.to(DEV) for t in norm_case(37, 640, BF16, F32, 4))
+    full, h, y, rstd = buffers(37, 640, E4M3), torch.empty_like(x), torch.empty_like(x), torch.empty(37, device=DEV)
+    q.quest_rms_norm_mx(x, w, 1e-5, 32, E4M3, residual=r, h_out=h, y_out=y, rstd=rstd, **full)
+    codes = buffers(37, 640, E4M3, mask=False)
+    h2, y2 = torch.empty_like(x), torch.empty_like(x)
+    wide_x, wide_r = torch.zeros(37, 656, dtype=BF16, device=DEV), torch.zeros(37, 672, dtype=BF16, device=DEV)
+    wide_x[:, :640], wide_r[:, :640] = x, r
+    q.quest_rms_norm_mx(wide_x[:, :640], w, 1e-5, 32, E4M3, residual=wide_r[:, :640], h_out=h2, **codes)
+    q.quest_rms_norm_mx(h2, w, 1e-5, y_out=y2)
+    assert torch.equal(h, h2) and torch.equal(y, y2)
+    assert torch.equal(full["codes"], codes["codes"]) and torch.equal(full["scales"], codes["scales"])
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-5])
+def test_norm_of_rows_without_a_number(eps):
+    """Zeros; a NaN or an infinity takes its row and no other."""
+    x, _, w = norm_case(5, 96, F32, F32, 8)
+    x[1] = 0
+    x[2, 7], x[3, 95] = float("nan"), float("inf")
+    got, y, rstd = buffers(5, 96, E4M3), torch.empty(5, 96, device=DEV), torch.empty(5, device=DEV)
+    q.quest_rms_norm_mx(x.to(DEV), w.to(DEV), eps, 32, E4M3, y_out=y, rstd=rstd, **got)
+    y, rstd, scales = y.cpu(), rstd.cpu(), host(got["scales"])
+    assert bool((y[1] == 0).all()) and (scales[1] == 0).all() and float(rstd[1]) == pytest.approx(0.0 if eps == 0 else eps ** -0.5)
+    assert bool(y[2:4].isnan().all()) and bool(rstd[2:4].isnan().all()) and (scales[2:4] == 255).all()
+    y64, _ = mx.rms_norm(x[[0, 4]].double().numpy(), w.double().numpy(), eps)
+    assert np.all(np.abs(y[[0, 4]].double().numpy() - y64) <= 64 * 2.0 ** -24 * np.abs(y64))
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 32), (3, 96), (777, 640), (2000, 2048), (5, 16384), (130, 5632), (9, 11008)])
+@pytest.mark.parametrize("dtype,weight_dtype", [(BF16, F32), (BF16, BF16), (F32, F32), (F32, BF16)])
+@pytest.mark.parametrize("along", [True, False])
+def test_norm_backward(rows, cols, dtype, weight_dtype, along):
+    h, dh, w = norm_case(rows, cols, dtype, weight_dtype, rows + cols)
+    dy = rows_of(rows, cols, dtype, 99, 0.03)
+    h64, w64, dy64 = h.double().numpy(), w.double().numpy(), dy.double().numpy()
+    rstd = torch.from_numpy(mx.rms_norm(h64, w64, 1e-5)[1].astype(np.float32))
+    dx, dw = torch.full((rows, cols), float("nan"), dtype=dtype, device=DEV), torch.full((cols,), float("nan"), device=DEV)
+    scratch = torch.full((q.quest_rms_norm_backward_workspace_bytes(rows, cols),), 0xC3, dtype=torch.uint8, device=DEV)
+    q.quest_rms_norm_backward(dy.to(DEV), h.to(DEV), w.to(DEV), rstd.to(DEV), dh=dh.to(DEV) if along else None, dx=dx, dweight=dw,
+                              workspace=scratch)
+    r64 = rstd.double().numpy()
+    dx64, dw64 = mx.rms_norm_backward(dy64, h64, w64, r64, dh.double().numpy() if along else None)
+    xhat, t = h64 * r64[:, None], dy64 * w64
+    # each of the cols terms of the mean rounds by 2^-24 four times at most before it is added, the sum once per addition
+    mean = (cols + 4) * 2.0 ** -24 * np.abs(t * xhat).mean(-1, keepdims=True)
+    fp32 = r64[:, None] * (8 * 2.0 ** -24 * (np.abs(t) + np.abs(xhat * (t * xhat).mean(-1, keepdims=True))) + np.abs(xhat) * mean)
+    assert np.all(np.abs(to_host_f64(dx) - dx64) <= fp32 + (HALF[dtype] + 2.0 ** -24) * np.abs(dx64))
+    assert np.all(np.abs(to_host_f64(dw) - dw64) <= (rows + 4) * 2.0 ** -24 * np.abs(dy64 * xhat).sum(0))
+    alone = torch.empty_like(dx)
+    q.quest_rms_norm_backward(dy.to(DEV), h.to(DEV), w.to(DEV), rstd.to(DEV), dh=dh.to(DEV) if along else None, dx=alone,
+                              dweight=None)
+    assert torch.equal(alone, dx)
+
+
+def test_norm_backward_against_differences():
+    """The gradient of sum(dy * y) against central differences of the 64-bit norm."""
+    h, _, w = norm_case(3, 64, F32, F32, 2)
+    dy = rows_of(3, 64, F32, 5)
+    h64, w64, dy64 = h.double().numpy(), w.double().numpy(), dy.double().numpy()
+    rstd = torch.from_numpy(mx.rms_norm(h64, w64, 1e-5)[1].astype(np.float32)).to(DEV)
+    dx, dw = torch.empty(3, 64, device=DEV), torch.empty(64, device=DEV)
+    scratch = torch.empty(q.quest_rms_norm_backward_workspace_bytes(3, 64), dtype=torch.uint8, device=DEV)
+    q.quest_rms_norm_backward(dy.to(DEV), h.to(DEV), w.to(DEV), rstd, dx=dx, dweight=dw, workspace=scratch)
+    loss = lambda a, b: (dy64 * mx.rms_norm(a, b, 1e-5)[0]).sum()  # noqa: E731
+    for i, j in ((0, 0), (1, 17), (2, 63)):
+        step = 1e-5 * max(abs(h64[i, j]), np.sqrt((h64[i] ** 2).mean()))
+        up, down = h64.copy(), h64.copy()
+        up[i, j] += step
+        down[i, j] -= step
+        slope = (loss(up, w64) - loss(down, w64)) / (2 * step)
+        size = np.abs(dy64[i] * w64).max() / np.sqrt((h64[i] ** 2).mean())
+        assert abs(float(dx[i, j]) - slope) <= 1e-5 * size
+        up, down = w64.copy(), w64.copy()
+        up[j] += 1e-3
+        down[j] -= 1e-3
+        assert abs(float(dw[j]) - (loss(h64, up) - loss(h64, down)) / 2e-3) <= 1e-5 * np.abs(dy64).max() * 10
+
+
+def test_norm_backward_without_rows():
+    dw = torch.full((640,), float("nan"), device=DEV)
+    none = torch.empty(0, 640, dtype=BF16, device=DEV)
+    q.quest_rms_norm_backward(none, none, torch.ones(640, device=DEV), torch.empty(0, device=DEV), dx=none.clone(), dweight=dw)
+    assert bool((dw == 0).all())
+
+
+# ---- together
+
+def layer_step(x, residual, w, norm_weight, dy, dh, block, fmt):
+    """A layer's training step: norm and quantizer, product, both gradients, both masked inverse transforms, the norm's."""
+    M, K, N = x.shape[0], x.shape[1], w.shape[0]
+    empty = lambda *s, dtype=BF16: torch.empty(*s, dtype=dtype, device=DEV)  # noqa: E731
+    xq, wq = buffers(M, K, fmt), buffers(N, K, E2M1)
+    t = dict(h=empty(M, K), rstd=empty(M, dtype=F32), y=empty(M, N), gx=empty(M, K), gw=empty(N, K), dn=empty(M, K), dw=empty(N, K),
+             dx=empty(M, K), dnorm=empty(K, dtype=F32))
+    scratch = torch.empty(max(q.quest_grad_gemm_mx_workspace_bytes(i, M, N, K) for i in (0, 1)), dtype=torch.uint8, device=DEV)
+    norm_scratch = torch.empty(q.quest_rms_norm_backward_workspace_bytes(M, K), dtype=torch.uint8, device=DEV)
+
+    def step():
+        q.quest_rms_norm_mx(x, norm_weight, 1e-5, block, fmt, residual=residual, h_out=t["h"], rstd=t["rstd"], **xq)
+        q.quest_hadamard_quantize_mx(w, block, E2M1, **wq)
+        q.quest_lowbit_gemm_mx(xq["codes"], xq["scales"], fmt, wq["codes"], wq["scales"], K, y=t["y"])
+        q.quest_grad_gemm_mx(0, dy, wq["codes"], wq["scales"], E2M1, M, N, K, out=t["gx"], workspace=scratch)
+        q.quest_grad_gemm_mx(1, dy, xq["codes"], xq["scales"], fmt, M, N, K, out=t["gw"], workspace=scratch)
+        q.quest_trust_backward_pair(t["gx"], xq["mask"], t["gw"], wq["mask"], block, out_x=t["dn"], out_w=t["dw"])
+        q.quest_rms_norm_backward(t["dn"], t["h"], norm_weight, t["rstd"], dh=dh, dx=t["dx"], dweight=t["dnorm"],
+                                  workspace=norm_scratch)
+    return step, t, xq, wq
+
+
+def step_inputs(M, N, K, seed):
+    x, residual, norm_weight = (t.to(DEV) for t in norm_case(M, K, BF16, F32, seed))
+    w, dy, dh = (rows_of(r, c, BF16, seed + i, s).to(DEV) for i, (r, c, s) in enumerate(((N, K, 0.02), (M, N, 0.03), (M, K, 0.03))))
+    return x, residual, w, norm_weight, dy, dh
+
+
+@pytest.mark.parametrize("fmt", [E2M1, E4M3])
+def test_training_step(fmt):
+    M, N, K, block = 320, 192, 256, 32
+    x, residual, w, norm_weight, dy, dh = step_inputs(M, N, K, 11)
+    step, t, xq, wq = layer_step(x, residual, w, norm_weight, dy, dh, block, fmt)
+    step()
+    # every operator's reference from what the one before left
+    a, b = (mx.values(host(o["codes"]), host(o["scales"]), f) for o, f in ((xq, fmt), (wq, E2M1)))
+    d = to_host_f64(dy)
+    for got, ref, slack in ((t["y"], a @ b.T, product_bound(a, b, fmt)), (t["gx"], d @ b, N * 2.0 ** -23 * (np.abs(d) @ np.abs(b))),
+                            (t["gw"], d.T @ a, M * 2.0 ** -23 * (np.abs(d).T @ np.abs(a)))):
+        assert np.all(np.abs(to_host_f64(got) - ref) <= 2.0 ** -8 * np.abs(ref) + slack)
+    h64, w64 = to_host_f64(t["h"]), to_host_f64(norm_weight)
+    dn = qo.trust_backward(to_host_f64(t["gx"]), qo.unpack_mask(host(xq["mask"]), K), block)
+    dx, dnorm = mx.rms_norm_backward(dn, h64, w64, to_host_f64(t["rstd"]), to_host_f64(dh))
+    # dn is rounded to bf16 on the way: 2^-8 of it reaches dx and dnorm, dx rounds once more
+    scale = to_host_f64(t["rstd"])[:, None] * np.abs(w64) * (np.abs(dn) + np.abs(dn).max(-1, keepdims=True))
+    assert np.all(np.abs(to_host_f64(t["dx"]) - dx) <= 2.0 ** -8 * 1.01 * np.abs(dx) + 2.0 ** -8 * 4 * scale)
+    size = (np.abs(dn * h64) * to_host_f64(t["rstd"])[:, None]).sum(0)
+    assert np.all(np.abs(to_host_f64(t["dnorm"]) - dnorm) <= 2.0 ** -8 * 1.1 * size)
+
+
+def test_captured_step_on_another_stream():
+    """A captured training step, replayed with eager work between the replays, gives the eager step's bits every time."""
+    M, N, K, block = 512, 256, 640, 128
+    inputs = step_inputs(M, N, K, 3)
+    step, t, xq, wq = layer_step(*inputs, block, E4M3)
+    q.quest_init()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    for seed in (4, 5, 6):
+        for mine, new in zip(inputs, step_inputs(M, N, K, seed)):
+            mine.copy_(new)
+        step()
+        torch.cuda.synchronize()
+        expected = {k: v.clone() for k, v in {**t, **xq}.items()}
+        for v in {**t, **xq}.values():
+            v.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k, v in {**t, **xq}.items():
+            assert torch.equal(v, expected[k]), k
+
+
+def test_decoding_step():
+    """One token's norm, quantizer and product by the calls of a serving step, against the same from 64 bits."""
+    K, N = 2048, 640
+    x, residual, norm_weight = (t.to(DEV) for t in norm_case(1, K, BF16, BF16, 21))
+    w = rows_of(N, K, BF16, 22, 0.02).to(DEV)
+    xq, wq = buffers(1, K, E4M3, mask=False), buffers(N, K, E2M1, mask=False)
+    h, y = torch.empty_like(x), torch.empty(1, N, dtype=BF16, device=DEV)
+    q.quest_hadamard_quantize_mx(w, 32, E2M1, **wq)
+    q.quest_rms_norm_mx(x, norm_weight, 1e-5, 32, E4M3, residual=residual, h_out=h, **xq)
+    q.quest_lowbit_gemm_mx(xq["codes"], xq["scales"], E4M3, wq["codes"], wq["scales"], K, y=y)
+    a, b = mx.values(host(xq["codes"]), host(xq["scales"]), E4M3), mx.values(host(wq["codes"]), host(wq["scales"]), E2M1)
+    ref = a @ b.T
+    assert np.all(np.abs(to_host_f64(y) - ref) <= 2.0 ** -8 * np.abs(ref) + product_bound(a, b, E4M3))
+    # and the whole against the unquantized layer: two roundings to elements, 2^-4 and 2^-2 of a value each, which average out
+    plain = (mx.rms_norm(to_host_f64(h), to_host_f64(norm_weight), 1e-5)[0] @ to_host_f64(w).T)
+    assert np.linalg.norm(ref - plain) <= 0.25 * np.linalg.norm(plain)

@@ -1,0 +1,237 @@
+"""Microscaled operands and the norm without a GPU: refusals of the C entry points and of the binding, and pins of the 64-bit
+definitions that the GPU tests compare with."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import microscaled as mx
+from paper_2502_05003_amd import binding as q
+
+FAKE, ODD = ctypes.c_void_p(0x10000), ctypes.c_void_p(0x10008)   # never dereferenced: validation fails first, or nothing to do
+OFF1, OFF2 = ctypes.c_void_p(0x10001), ctypes.c_void_p(0x10002)
+OK, NULL, SHAPE, BLOCK, ALIGN, DTYPE, ARG = 0, 1, 2, 4, 5, 6, 8
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return q.load()
+
+
+def test_quantizer_refuses(lib):
+    def call(x=FAKE, dtype=1, rows=0, cols=512, ld=512, n=32, fmt=0, codes=FAKE, scales=FAKE, mask=FAKE):
+        return lib.quest_hadamard_quantize_mx(x, dtype, rows, cols, ld, n, fmt, codes, scales, mask, None)
+    assert call() == OK and call(mask=None) == OK and call(x=None, codes=None, scales=None) == OK and call(scales=OFF1) == OK
+    for missing in ("x", "codes", "scales"):
+        assert call(rows=4, **{missing: None}) == NULL
+    assert call(dtype=2) == DTYPE and call(fmt=2) == DTYPE and call(fmt=-1) == DTYPE
+    for cols in (0, 16, 31, 40, 16416, -32):
+        assert call(cols=cols, ld=32768) == SHAPE
+    assert call(rows=-1) == SHAPE and call(ld=480) == SHAPE and call(rows=1 << 24) == SHAPE
+    assert call(rows=(1 << 24) - 1, cols=2048, ld=2048) == SHAPE          # more than 2^34 elements
+    for n in (0, -1, 3, 48, 1024, 32768):
+        assert call(n=n) == BLOCK
+    assert call(cols=96, n=64) == BLOCK
+    assert call(x=ODD) == ALIGN and call(codes=ODD) == ALIGN and call(mask=OFF1) == ALIGN and call(ld=516) == ALIGN
+    assert call(ld=516, dtype=0) == OK and call(ld=518, dtype=0) == ALIGN
+
+
+def test_reading_back_refuses(lib):
+    def call(codes=FAKE, scales=FAKE, fmt=1, rows=0, cols=512, out=FAKE, dtype=1, ld=512):
+        return lib.quest_dequantize_mx(codes, scales, fmt, rows, cols, out, dtype, ld, None)
+    assert call() == OK and call(codes=None) == OK
+    assert call(rows=1, codes=None) == NULL and call(rows=1, scales=None) == NULL and call(rows=1, out=None) == NULL
+    assert call(fmt=3) == DTYPE and call(dtype=5) == DTYPE
+    assert call(cols=48) == SHAPE and call(ld=511) == SHAPE and call(rows=-3) == SHAPE
+    assert call(codes=ODD) == ALIGN and call(out=OFF2) == ALIGN and call(ld=516) == ALIGN
+
+
+def test_product_refuses(lib):
+    def call(a=FAKE, sa=FAKE, fmt=1, M=0, b=FAKE, sb=FAKE, N=8, K=512, y=FAKE, ld=8, acc=None):
+        return lib.quest_lowbit_gemm_mx(a, sa, fmt, M, b, sb, N, K, y, ld, acc, None)
+    assert call() == OK and call(M=8, N=0, ld=0) == OK and call(y=None) == OK and call(a=None) == OK
+    for missing in ("a", "sa", "b", "sb", "y"):
+        assert call(M=4, **{missing: None}) == NULL
+    assert call(fmt=2) == DTYPE
+    for K in (0, 64, 192, 65536 + 128, -128):
+        assert call(K=K) == SHAPE
+    assert call(M=-1) == SHAPE and call(N=-1) == SHAPE and call(M=(1 << 22) + 1) == SHAPE and call(N=(1 << 22) + 1) == SHAPE
+    assert call(ld=7) == SHAPE and call(ld=7, y=None, acc=FAKE) == OK
+    assert call(a=ODD) == ALIGN and call(b=ODD) == ALIGN and call(sa=OFF2) == ALIGN and call(sb=OFF1) == ALIGN
+    assert call(y=OFF1) == ALIGN and call(acc=OFF2) == ALIGN and call(y=OFF2) == OK
+
+
+def test_gradient_products_refuse(lib):
+    def call(which=0, dy=FAKE, c=FAKE, s=FAKE, fmt=0, M=512, N=256, K=512, out=FAKE, ws=FAKE, wsb=1 << 30):
+        return lib.quest_grad_gemm_mx(which, dy, c, s, fmt, M, N, K, out, ws, wsb, None)
+    for missing in ("dy", "c", "s", "out"):
+        assert call(**{missing: None}) == NULL
+    assert call(which=2) == ARG and call(which=-1) == ARG and call(fmt=2) == DTYPE
+    assert call(M=64) == SHAPE and call(M=520) == SHAPE and call(which=1, N=64) == SHAPE and call(K=64) == SHAPE
+    need = q.quest_grad_gemm_mx_workspace_bytes(0, 512, 256, 512)
+    assert need == 256 * 512 * 2 and q.quest_grad_gemm_mx_workspace_bytes(0, 64, 256, 512) == -1
+    assert q.quest_grad_gemm_mx_workspace_bytes(2, 512, 256, 512) == -1
+    assert call(ws=None, wsb=0) == ARG and call(wsb=need - 1) == ARG and call(wsb=-1) == ARG
+    assert call(dy=ODD) == ALIGN and call(c=ODD) == ALIGN and call(out=ODD) == ALIGN and call(ws=ODD) == ALIGN
+
+
+def test_norm_refuses(lib):
+    def call(x=FAKE, ldx=512, r=FAKE, ldr=512, dtype=1, w=FAKE, wd=0, rows=0, cols=512, eps=1e-5, h=FAKE, y=FAKE, n=32, fmt=1,
+             codes=FAKE, scales=FAKE, mask=FAKE, rstd=FAKE):
+        return lib.quest_rms_norm_mx(x, ldx, r, ldr, dtype, w, wd, rows, cols, eps, h, y, n, fmt, codes, scales, mask, rstd, None)
+    assert call() == OK and call(r=None, h=None, ldr=0) == OK and call(y=None, mask=None, rstd=None) == OK
+    none = dict(codes=None, scales=None, mask=None)
+    assert call(n=0, fmt=9, **none) == OK                       # not looked at without codes
+    assert call(rows=1, y=None, **none) == NULL and call(rows=1, x=None) == NULL and call(w=None) == NULL
+    assert call(dtype=2) == DTYPE and call(wd=2) == DTYPE and call(fmt=2) == DTYPE
+    assert call(cols=48) == SHAPE and call(ldx=511) == SHAPE and call(ldr=480) == SHAPE and call(rows=-1) == SHAPE
+    assert call(rows=1 << 24) == SHAPE
+    assert call(n=24) == BLOCK and call(cols=2048, ldx=2048, ldr=2048, n=1024) == BLOCK and call(cols=96, n=64) == BLOCK
+    for eps in (-1e-5, float("nan"), float("inf")):
+        assert call(eps=eps) == ARG
+    assert call(h=None) == ARG and call(r=None) == ARG          # the residual and what comes of it: both or neither
+    assert call(scales=None) == ARG and call(codes=None) == ARG and call(codes=None, scales=None) == ARG
+    for at in ("x", "r", "w", "h", "y", "codes", "mask"):
+        assert call(**{at: ODD}) == ALIGN
+    assert call(rstd=OFF2) == ALIGN and call(ldx=516) == ALIGN and call(ldr=516) == ALIGN and call(scales=OFF1) == OK
+
+
+def test_norm_backward_refuses(lib):
+    def call(dy=FAKE, h=FAKE, dtype=1, w=FAKE, wd=0, rstd=FAKE, dh=FAKE, rows=8, cols=512, dx=FAKE, dw=FAKE, ws=FAKE, wsb=1 << 30):
+        return lib.quest_rms_norm_backward(dy, h, dtype, w, wd, rstd, dh, rows, cols, dx, dw, ws, wsb, None)
+    for missing in ("dy", "h", "w", "rstd", "dx"):
+        assert call(**{missing: None}) == NULL
+    assert call(rows=0, dy=None, h=None, rstd=None, dx=None, dw=None) == OK
+    assert call(dtype=3) == DTYPE and call(wd=-1) == DTYPE
+    assert call(cols=40) == SHAPE and call(rows=-1) == SHAPE
+    need = q.quest_rms_norm_backward_workspace_bytes(8, 512)
+    assert need > 0 and q.quest_rms_norm_backward_workspace_bytes(8, 40) == -1 and q.quest_rms_norm_backward_workspace_bytes(-1, 64) == -1
+    assert call(ws=None, wsb=0) == ARG and call(wsb=need - 1) == ARG and call(wsb=-1) == ARG
+    for at in ("dy", "h", "w", "dh", "dx", "dw", "ws"):
+        assert call(**{at: ODD}) == ALIGN
+    assert call(rstd=OFF2) == ALIGN
+
+
+# ---- the binding's own checks (tensors on the CPU: everything else is refused before the place is looked at)
+
+def u8(*shape):
+    return torch.zeros(*shape, dtype=torch.uint8)
+
+
+def test_binding_refuses_other_shapes_types_and_places():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    good = dict(codes=u8(4, 32), scales=u8(4, 2), mask=u8(4, 8))
+    for changed in (dict(codes=u8(4, 64)), dict(codes=u8(4, 64)[:, ::2]), dict(scales=u8(4, 1)), dict(scales=torch.zeros(4, 2)),
+                    dict(mask=u8(4, 4)), dict(codes=u8(128))):
+        with pytest.raises(ValueError):
+            q.quest_hadamard_quantize_mx(x, 32, q.QUEST_MX_E2M1, **(good | changed))
+    with pytest.raises(ValueError, match="format"):
+        q.quest_hadamard_quantize_mx(x, 32, 7, **good)
+    with pytest.raises(ValueError, match="not contiguous"):
+        q.quest_hadamard_quantize_mx(torch.zeros(64, 4, dtype=torch.bfloat16).t(), 32, q.QUEST_MX_E2M1, **good)
+    with pytest.raises(ValueError):
+        q.quest_hadamard_quantize_mx(x[0], 32, q.QUEST_MX_E2M1, **good)
+    with pytest.raises(ValueError):
+        q.quest_dequantize_mx(u8(4, 32), u8(4, 2), q.QUEST_MX_E2M1, out=torch.zeros(4, 128))
+    a, s, b, t = u8(4, 128), u8(4, 4), u8(6, 64), u8(6, 4)
+    y = torch.zeros(4, 6, dtype=torch.bfloat16)
+    for args in ((a[:, :64], s, 1, b, t, 128), (a, s[:, :3], 1, b, t, 128), (a, s, 0, b, t, 128), (a, s, 1, u8(6, 128), t, 128)):
+        with pytest.raises(ValueError):
+            q.quest_lowbit_gemm_mx(*args, y=y)
+    with pytest.raises(ValueError):
+        q.quest_lowbit_gemm_mx(a, s, 1, b, t, 128, y=torch.zeros(6, 4, dtype=torch.bfloat16).t())
+    with pytest.raises(TypeError):
+        q.quest_lowbit_gemm_mx(a, s, 1, b, t, 128, y=torch.zeros(4, 6))
+    with pytest.raises(ValueError):
+        q.quest_lowbit_gemm_mx(a, s, 1, b, t, 128, y=None, acc_out=torch.zeros(4, 7))
+    dy = torch.zeros(128, 192, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        q.quest_grad_gemm_mx(0, dy, u8(192, 64), u8(192, 4), 0, 128, 192, 128, out=torch.zeros(192, 128, dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        q.quest_grad_gemm_mx(1, dy, u8(192, 64), u8(192, 4), 0, 128, 192, 128, out=torch.zeros(192, 128, dtype=torch.bfloat16))
+    w, rstd = torch.zeros(64), torch.zeros(4)
+    with pytest.raises(TypeError):
+        q.quest_rms_norm_mx(x, w, 1e-5, residual=x.float(), h_out=x.clone(), y_out=x.clone())
+    for changed in (dict(y_out=x.float()), dict(residual=x[:2], h_out=x), dict(rstd=rstd[:3], y_out=x), dict(y_out=x[:, :32])):
+        with pytest.raises(ValueError):
+            q.quest_rms_norm_mx(x, w, 1e-5, **changed)
+    with pytest.raises(ValueError):
+        q.quest_rms_norm_mx(x, w[:32], 1e-5, y_out=x.clone())
+    for changed in (dict(dx=x.float()), dict(dweight=w.double()), dict(dh=x[:, ::2]), dict(dh=x[:3])):
+        with pytest.raises(ValueError):
+            q.quest_rms_norm_backward(x, x, w, rstd, **(dict(dx=x.clone(), dweight=w.clone()) | changed))
+
+
+def test_binding_refuses_tensors_elsewhere(monkeypatch):
+    """Host memory must not reach a kernel."""
+    monkeypatch.setattr(q, "_current_device", lambda: 0)
+    x, w, rstd = torch.zeros(128, 128, dtype=torch.bfloat16), torch.zeros(128), torch.zeros(128)
+    codes, scales = u8(128, 64), u8(128, 4)
+    for call in (lambda: q.quest_hadamard_quantize_mx(x, 32, 0, codes=codes, scales=scales),
+                 lambda: q.quest_dequantize_mx(codes, scales, 0, out=x),
+                 lambda: q.quest_lowbit_gemm_mx(codes, scales, 0, codes, scales, 128, y=x),
+                 lambda: q.quest_grad_gemm_mx(0, x, codes, scales, 0, 128, 128, 128, out=x),
+                 lambda: q.quest_rms_norm_mx(x, w, 1e-5, 32, 0, codes=codes, scales=scales),
+                 lambda: q.quest_rms_norm_backward(x, x, w, rstd, dx=x, dweight=None)):
+        with pytest.raises(ValueError, match="is on cpu"):
+            call()
+
+
+# ---- the definitions
+
+def test_element_grids():
+    assert mx.MAGNITUDES[0].tolist() == [0, 0.5, 1, 1.5, 2, 3, 4, 6]
+    e4m3 = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(mx.MAGNITUDES[1], e4m3) and mx.TRUSTED == (7.0, 464.0)
+
+
+def test_hand_checked_group():
+    g = np.zeros((1, 32))
+    g[0, :12] = [6, 5, 3.5, 2.5, 1.75, 1.25, 0.75, 0.25, -0.25, -5, -6, 0.3]
+    code, scales, trust = mx.quantize(g, 0)
+    assert scales[0, 0] == 127 and trust.all()
+    assert code[0, :13].tolist() == [7, 6, 6, 4, 4, 2, 2, 0, 8, 14, 15, 1, 0]
+    code, scales, trust = mx.quantize(g * 1.25, 0)                 # 7.5: clipped, beyond the trust border; 6.25 is within it
+    assert scales[0, 0] == 127 and code[0, :2].tolist() == [7, 7] and trust[0, :3].tolist() == [False, True, True]
+    code, scales, _ = mx.quantize(g * 4 / 3, 0)                    # 8: the next binade
+    assert scales[0, 0] == 128 and code[0, 0] == 6
+    zero = mx.quantize(np.zeros((1, 32)), 1)
+    assert zero[1][0, 0] == 0 and not zero[0].any() and zero[2].all()
+    g[0, 3] = np.nan
+    code, scales, trust = mx.quantize(np.concatenate([g, g * 0 + 1], axis=1), 1)
+    assert scales[0].tolist() == [255, 255] and not trust.any()
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_quantized_values_are_the_nearest(fmt):
+    x = np.random.default_rng(fmt).standard_normal((64, 96))
+    code, scales, trust = mx.quantize(x, fmt)
+    v = mx.values(mx.pack(code, fmt), scales, fmt)
+    scale = np.repeat(np.ldexp(1.0, scales.astype(int) - 127), 32, axis=1)
+    grid = np.concatenate([mx.MAGNITUDES[fmt], -mx.MAGNITUDES[fmt]])
+    for r in range(8):
+        assert np.allclose(np.abs(v[r] - x[r]), np.abs(grid[:, None] * scale[r] - x[r]).min(0), rtol=1e-12, atol=1e-300)
+    largest = np.abs(x).reshape(64, 3, 32).max(-1)
+    top = mx.MAGNITUDES[fmt][-1]
+    assert np.all(largest / np.ldexp(1.0, scales.astype(int) - 127) < 2.0 ** (mx.LARGEST_EXPONENT[fmt] + 1))
+    assert np.all(np.abs(v)[~trust] == (top * scale)[~trust])
+
+
+def test_transform_in_fp32_is_the_transform():
+    from oracle import quest_oracle as qo
+    x = np.random.default_rng(0).standard_normal((3, 512)).astype(np.float32)
+    for n in (1, 2, 32, 512):
+        assert np.allclose(mx.hadamard_f32(x, n), qo.hadamard(x.astype(np.float64), n), rtol=0, atol=2e-6)
+
+
+def test_norm_gradient_against_differences():
+    rng = np.random.default_rng(3)
+    h, w, dy = rng.standard_normal((2, 32)), rng.standard_normal(32), rng.standard_normal((2, 32))
+    dx, dw = mx.rms_norm_backward(dy, h, w, mx.rms_norm(h, w, 1e-3)[1])
+    loss = lambda a, b: (dy * mx.rms_norm(a, b, 1e-3)[0]).sum()  # noqa: E731
+    for j in range(0, 32, 5):
+        step = np.zeros((2, 32))
+        step[1, j] = 1e-6
+        assert dx[1, j] == pytest.approx((loss(h + step, w) - loss(h - step, w)) / 2e-6, rel=1e-6, abs=1e-8)
+        assert dw[j] == pytest.approx((loss(h, w + step[1]) - loss(h, w - step[1])) / 2e-6, rel=1e-6, abs=1e-8)
