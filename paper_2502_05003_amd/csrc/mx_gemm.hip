@@ -3,6 +3,8 @@
 //
 // Operands of the instruction, K = 128: lane l holds row l % 16 of its operand and the scale byte of the elements 32 q .. + 32,
 // q = l / 16.  E2M1: those 32 elements, 16 bytes.  E4M3: elements 16 q .. + 16 and 64 + 16 q .. + 16, 16 bytes each.
+#include <algorithm>
+
 #include "mx_formats.h"
 #include "quest_internal.h"
 
@@ -141,9 +143,433 @@ hipError_t launch_few(const MxGemmArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
+// ------------------------------------------------------------------------------------------
+// Outputs of many tiles.  A workgroup of four waves works through tiles of 64 WI x 64 WJ outputs, each wave 32 WI x 32 WJ of them
+// in accumulation registers, as one stream of stages: 128 bytes of each activation row (256 elements in E2M1, 128 in E4M3), whole
+// cache lines, and the same elements of the weights.  Two stages of LDS, filled by direct transfers.
+//
+// A stage is multiplied block of 32 rows by block: the wave's weight fragments of the whole stage stay in registers, the
+// activations' come one block ahead.  The last block of a stage runs behind the barrier that announces the next one:
+//   barrier: the stage has landed, the other buffer has been left by all waves
+//   phase 1   multiply block WI - 1 of the stage before; each weight fragment that is done with is replaced by the new stage's
+//   phase 2   block 0 of the stage;  phase 3 ..  blocks 1 .. WI - 2
+//   wait for the reads of block WI - 1 and for the next stage's transfers, which phases 1 and 2 have issued; barrier
+// Nothing but the waits for these two interrupts the matrix instructions, tile ends included: the transfers run on into the
+// workgroup's next tile, whose first products start from zero (C = 0, no accumulator is cleared), and block b of a finished
+// tile is rounded, parked in the wave's corner of LDS and stored as whole row segments while block b + 1 is multiplied.
+// ------------------------------------------------------------------------------------------
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+constexpr int kTileThreads = 256;
+constexpr int kParkBytes = 32 * 128;       // 32 rows by 64 columns in bf16
+constexpr int kScaleChunk = 512;           // elements whose scales one transfer of 16 bytes per row brings
+
+template <int FORMAT, int WI, int WJ>
+struct MxTile {
+    static constexpr bool kE4M3 = FORMAT == QUEST_MX_E4M3;
+    static constexpr int kRows = 64 * WI, kCols = 64 * WJ;
+    static constexpr int kSteps = kE4M3 ? 2 : 4;                 // matrix instructions along a stage (64 elements each)
+    static constexpr int kStageK = 64 * kSteps;
+    static constexpr int kRowA = 128, kRowB = 32 * kSteps;       // bytes of a row in a stage
+    static constexpr int kBytesA = kRows * kRowA, kStage = kBytesA + kCols * kRowB;
+    static constexpr int kScales = (kRows + kCols) * 16;
+    static constexpr int kLds = 2 * kStage + 2 * kScales + 4 * kParkBytes;
+    static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
+};
+
+// what an iteration (a stage) of the stream is
+enum {
+    kStageFirst = 1,      // the first of its tile: the tile before ends in phase 1
+    kAfterFirst = 2,      // the one behind it
+    kStageLast = 4        // the last of its tile
+};
+
+// One piece of 32 rows by 64 columns, parked with 16-byte chunk c of row r at c ^ (r & 7), where whole 16-byte stores do not do
+__device__ __forceinline__ void store_ragged_piece(const uint8_t *park, uint16_t *__restrict__ y, int64_t ld_y, int row0, int col0,
+                                                int M, int N, int lane)
+{
+    uint16_t *const base = y + (int64_t)row0 * ld_y + col0;
+    auto parked = [&](int row, int col) { return park + row * 128 + (((col >> 3) ^ (row & 7)) << 4) + (col & 7) * 2; };
+    if ((ld_y & 7) == 0 && (reinterpret_cast<uintptr_t>(y) & 15) == 0) {
+        const int c = 8 * (lane & 7), left = N - col0 - c;
+        for (int row = lane >> 3; row < 32 && row0 + row < M; row += 8) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(parked(row, c));
+            uint16_t *dst = base + (int64_t)row * ld_y + c;
+            if (left >= 8) {
+                *reinterpret_cast<uint4 *>(dst) = v;
+            } else {
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (e < left)
+                        dst[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+            }
+        }
+        return;
+    }
+    if ((ld_y & 1) == 0 && (reinterpret_cast<uintptr_t>(y) & 3) == 0) {   // consecutive columns, two to a lane
+        const int c = 2 * (lane & 31);
+        for (int row = lane >> 5; row < 32 && row0 + row < M; row += 2) {
+            const uint32_t v = *reinterpret_cast<const uint32_t *>(parked(row, c));
+            uint16_t *dst = base + (int64_t)row * ld_y + c;
+            if (col0 + c + 1 < N)
+                *reinterpret_cast<uint32_t *>(dst) = v;
+            else if (col0 + c < N)
+                *dst = (uint16_t)v;
+        }
+        return;
+    }
+    for (int row = 0; row < 32 && row0 + row < M; ++row)
+        if (col0 + lane < N)
+            base[(int64_t)row * ld_y + lane] = *reinterpret_cast<const uint16_t *>(parked(row, lane));
+}
+
+// TWO: tiles of two stages (else more); GENERAL: rows of y that 16-byte stores do not fit, or raw accumulators
+template <int FORMAT, int WI, int WJ, bool TWO, bool GENERAL>
+__global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
+    const uint8_t *__restrict__ a_codes, const uint8_t *__restrict__ a_scales, const uint8_t *__restrict__ b_codes,
+    const uint8_t *__restrict__ b_scales, int M, int N, int K, int tiles_m, int tiles_n, uint16_t *__restrict__ y, int64_t ld_y,
+    float *__restrict__ acc_out)
+{
+    typedef MxTile<FORMAT, WI, WJ> T;
+    constexpr bool kE4M3 = T::kE4M3;
+    constexpr int SS = T::kSteps, kFragB = SS * WJ;      // weight fragments of a stage, matrix instructions of a phase
+    constexpr int nA = 2 * WI, nB = T::kCols * T::kRowB / 4096, kDma = nA + nB;   // transfers of a wave and stage
+    constexpr int kScaleWords = SS / 2;                  // scale dwords of a row and stage
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+
+    // Tiles of this workgroup: each XCD (workgroup ids go to the eight in turn) has one contiguous run of tiles, ordered four
+    // tile-rows deep, of which its workgroups take every (number of workgroups)-th.
+    const int total = tiles_m * tiles_n, per_xcd = (total + 7) / 8, peers = gridDim.x / 8;
+    const int xcd = blockIdx.x & 7, run_end = min((xcd + 1) * per_xcd, total);
+    int tile = xcd * per_xcd + (blockIdx.x >> 3);
+    if (tile >= run_end)
+        return;
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave >> 1, wc = wave & 1;
+    const int lm = lane & 31, lh = lane >> 5;
+    const uint32_t smem_addr = lds_address(smem);
+    const int64_t row_a = kE4M3 ? K : K / 2, row_b = K / 2;
+    const int row_scales = K / 32;                       // bytes
+    const int stages = (K + T::kStageK - 1) / T::kStageK;
+    const bool half_stage = K % T::kStageK != 0;         // E2M1: the last stage of a tile holds 128 elements
+    const int words = K / 128;                           // scale dwords of a row
+
+    // ---- transfers, one stage ahead of the multiplication
+    uint32_t voff[kDma], scale_voff[2];
+    const uint8_t *fetch_a, *fetch_b, *fetch_as, *fetch_bs;   // the fetched tile's rows (wave-uniform)
+    auto set_fetch_tile = [&](int at, int &m0, int &n0) __attribute__((always_inline)) {
+        const int band = at / (4 * tiles_n), band_rows = min(4, tiles_m - band * 4), in_band = at - band * 4 * tiles_n;
+        m0 = __builtin_amdgcn_readfirstlane((band * 4 + in_band % band_rows) * T::kRows);
+        n0 = __builtin_amdgcn_readfirstlane(in_band / band_rows * T::kCols);
+        const int last_a = M - 1 - m0, last_b = N - 1 - n0;   // rows beyond the edge: the last row again, not stored
+        fetch_a = a_codes + m0 * row_a;
+        fetch_b = b_codes + n0 * row_b;
+        fetch_as = a_scales + (int64_t)m0 * row_scales;
+        fetch_bs = b_scales + (int64_t)n0 * row_scales;
+        // a transfer moves 1 KiB: lane l lands at 16 l, so it fetches the chunk that belongs there (see the reads below)
+#pragma unroll
+        for (int p = 0; p < kDma; ++p) {
+            const bool left = p < nA;
+            const int piece = left ? wave * nA + p : wave * nB + p - nA;
+            if (left || T::kRowB == 128) {
+                const int row = piece * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
+                voff[p] = (uint32_t)min(row, left ? last_a : last_b) * (uint32_t)(left ? row_a : row_b) + 16u * chunk;
+            } else {
+                const int row = piece * 16 + (lane >> 2), chunk = (lane & 3) ^ ((row >> 2) & 3);
+                voff[p] = (uint32_t)min(row, last_b) * (uint32_t)row_b + 16u * chunk;
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int piece = wave + 4 * h;
+            scale_voff[h] = (uint32_t)(piece < WI ? min(64 * piece + lane, last_a) : min(64 * (piece - WI) + lane, last_b)) *
+                            (uint32_t)row_scales;
+        }
+    };
+    // lanes whose chunk lies in the second half of a row's 128 bytes, which a half stage does not have: they fetch the first again
+    const uint32_t back[2] = {(lane & 4) ? 64u : 0u, (lane & 4) ? 0u : 64u};
+    auto transfer = [&](auto pc, uint32_t stage, int at, bool half) __attribute__((always_inline)) {
+        constexpr int p = decltype(pc)::value;
+        constexpr bool left = p < nA;
+        const uint32_t off = !kE4M3 && half ? voff[p] - back[p & 1] : voff[p];
+        if constexpr (left)
+            lds_dma16_at<1024 * p>(fetch_a + at * T::kRowA, off, stage + wave * (nA * 1024));
+        else
+            lds_dma16_at<T::kBytesA + 1024 * (p - nA)>(fetch_b + at * T::kRowB, off, stage + wave * (nB * 1024));
+    };
+    const uint32_t scale_addr = smem_addr + 2 * T::kStage;
+    // first scale dword of the 16 bytes that hold a stage's (the last ones of a row end where the row ends)
+    auto chunk_start = [&](int at) { return min(at * T::kStageK / kScaleChunk * 4, words - 4); };
+    auto transfer_scales = [&](int buffer, int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int piece = wave + 4 * h;
+            if (piece < WI + WJ)
+                lds_dma16((piece < WI ? fetch_as : fetch_bs) + 4 * chunk_start(at), scale_voff[h],
+                          scale_addr + buffer * T::kScales + piece * 1024);
+        }
+    };
+
+    // ---- fragments.  Chunk c of row r of 128 bytes sits at c ^ ((r >> 1) & 7) (64 bytes: c ^ ((r >> 2) & 3)): sixteen
+    // consecutive rows then meet sixteen different 16-byte slots modulo 256 bytes.
+    //   E2M1, step ss: chunk 2 ss + lh;  E4M3: chunks 4 ss + lh and 4 ss + 2 + lh
+    uint4 af[2][4], bf[kFragB];            // activations: [block & 1][quarter of the 128 bytes]
+    uint32_t sa[WI][kScaleWords], sb[WJ][kScaleWords];
+    const uint32_t a_lane = (wr * 32 * WI + lm) * T::kRowA + ((lh ^ ((lm >> 1) & 7)) << 4);
+    const uint32_t b_lane = T::kBytesA + (wc * 32 * WJ + lm) * T::kRowB +
+                            ((T::kRowB == 128 ? lh ^ ((lm >> 1) & 7) : lh ^ ((lm >> 2) & 3)) << 4);
+    auto read_a = [&](const uint8_t *stage, auto block, auto quarter) __attribute__((always_inline)) {
+        constexpr int i = decltype(block)::value, c = decltype(quarter)::value;
+        af[i & 1][c] = *reinterpret_cast<const uint4 *>(stage + (a_lane ^ (c << 5)) + i * 32 * T::kRowA);
+    };
+    auto read_b = [&](const uint8_t *stage, auto frag) __attribute__((always_inline)) {
+        constexpr int f = decltype(frag)::value, ss = f / WJ, j = f % WJ;
+        bf[f] = *reinterpret_cast<const uint4 *>(stage + (b_lane ^ (ss << 5)) + j * 32 * T::kRowB);
+    };
+    // (shifted so that byte 0 is the lane's group of step 0, byte 2 that of step 1)
+    auto read_scale = [&](int buffer, int word, int row) __attribute__((always_inline)) {
+        return *reinterpret_cast<const uint32_t *>(smem + 2 * T::kStage + buffer * T::kScales + row * 16 + word * 4) >> (8 * lh);
+    };
+
+    v16f acc[WI][WJ];
+    // matrix instruction f of block i: the weights are the row operand, so a lane's sums are four runs of consecutive outputs
+    auto multiply = [&](auto block, auto frag, auto from_zero, const uint32_t (&scale_a)[kScaleWords]) __attribute__((always_inline)) {
+        constexpr int i = decltype(block)::value, f = decltype(frag)::value, ss = f / WJ, j = f % WJ;
+        constexpr bool zero = decltype(from_zero)::value && ss == 0;
+        const v8i b = v8i{(int)bf[f].x, (int)bf[f].y, (int)bf[f].z, (int)bf[f].w, 0, 0, 0, 0};
+        v8i a;
+        if constexpr (kE4M3) {
+            const uint4 &lo = af[i & 1][2 * ss], &hi = af[i & 1][2 * ss + 1];
+            a = v8i{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+        } else {
+            const uint4 &lo = af[i & 1][ss];
+            a = v8i{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, 0, 0, 0, 0};
+        }
+        const v16f c = zero ? v16f{} : acc[i][j];
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, c, kF4, kE4M3 ? kF8 : kF4, 2 * (ss & 1),
+                                                                    (int)sb[j][ss / 2], 2 * (ss & 1), (int)scale_a[ss / 2]);
+    };
+
+    // ---- the output of a finished tile
+    int out_m = 0, out_n = 0;              // this wave's part of it
+    uint8_t *const park = smem + 2 * T::kStage + 2 * T::kScales + wave * kParkBytes;
+    const uint32_t y_lane = (uint32_t)(lane >> 3) * (uint32_t)ld_y * 2u + 16u * (lane & 7);
+    quest_v4u out_reg[4];
+    // Part n of kOutParts of storing block i; the block has WJ / 2 pieces of 64 columns, a piece four writes, one read, one store.
+    constexpr int kOutParts = (WJ / 2) * 6;
+    auto store_part = [&](auto block, auto part) __attribute__((always_inline)) {
+        constexpr int i = decltype(block)::value, piece = decltype(part)::value / 6, n = decltype(part)::value % 6;
+        if constexpr (GENERAL && n == 0 && piece == 0) {
+            if (acc_out)
+                static_for<WJ>([&](auto jc) {
+                    constexpr int j = decltype(jc)::value;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int m = out_m + 32 * i + lm, col = out_n + 32 * j + 8 * (r >> 2) + 4 * lh + (r & 3);
+                        if (m < M && col < N)
+                            acc_out[(int64_t)m * N + col] = acc[i][j][r];
+                    }
+                });
+        }
+        if constexpr (n < 4) {             // columns 16 n .. + 16 of the piece
+            constexpr int j = 2 * piece + n / 2;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int g = 2 * (n & 1) + h;
+                *reinterpret_cast<uint2 *>(park + lm * 128 + (((4 * (n / 2) + g) ^ (lm & 7)) << 4) + 8 * lh) =
+                    make_uint2(pack_bf16(acc[i][j][4 * g], acc[i][j][4 * g + 1]), pack_bf16(acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]));
+            }
+        } else if constexpr (GENERAL) {
+            if (n == 5 && y && out_m + 32 * i < M && out_n + 64 * piece < N)
+                store_ragged_piece(park, y, ld_y, out_m + 32 * i, out_n + 64 * piece, M, N, lane);
+        } else if constexpr (n == 4) {
+#pragma unroll
+            for (int pass = 0; pass < 4; ++pass) {
+                const int row = 8 * pass + (lane >> 3);
+                out_reg[pass] = *reinterpret_cast<const quest_v4u *>(park + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+            }
+        } else {
+            // rows and columns that do not exist lie outside of the buffer (columns come in eights)
+            const int rows = min(max(M - out_m - 32 * i, 0), 32);
+            const auto buffer = __builtin_amdgcn_make_buffer_rsrc(y + (int64_t)(out_m + 32 * i) * ld_y + out_n + 64 * piece, 0,
+                                                                  rows * (int)ld_y * 2, 0x00027000);
+            const uint32_t at = out_n + 64 * piece + 8 * (lane & 7) < N ? y_lane : 0x80000000u;
+#pragma unroll
+            for (int pass = 0; pass < 4; ++pass)
+                __builtin_amdgcn_raw_buffer_store_b128(out_reg[pass], buffer, (int)(at + (uint32_t)(8 * pass) * (uint32_t)ld_y * 2u), 0, 0);
+        }
+    };
+
+    int cur = 0, scale_buffer = 0;         // where the stage being multiplied is
+    int m0, n0, next_m0 = 0, next_n0 = 0;
+    // One stage: number `at` of the tile; the stage behind it is fetched
+    auto iteration = [&](auto kind, int at) __attribute__((always_inline)) {
+        constexpr int k = decltype(kind)::value;
+        constexpr bool last = (k & kStageLast) != 0, boundary = (k & kStageFirst) != 0;
+        const uint8_t *stage = smem + cur * T::kStage;
+        const uint32_t refill = smem_addr + (cur ^ 1) * T::kStage;
+        if constexpr (last) {
+            if (tile + peers < run_end)    // else the tile's first stage again, not used
+                set_fetch_tile(tile + peers, next_m0, next_n0);
+        }
+        const int fetched = last ? 0 : at + 1;
+        const bool fetched_half = !kE4M3 && half_stage && fetched == stages - 1;
+        const bool new_scales = fetched * T::kStageK % kScaleChunk == 0;
+        if (new_scales)
+            transfer_scales(scale_buffer ^ 1, fetched);
+        // this stage's scales; those of the block that phase 1 finishes stay until then
+        uint32_t sa_before[kScaleWords], sb_new[WJ][kScaleWords];
+        const int word = at * (T::kStageK / 128) - chunk_start(at);
+#pragma unroll
+        for (int w = 0; w < kScaleWords; ++w) {
+            sa_before[w] = sa[WI - 1][w];
+#pragma unroll
+            for (int i = 0; i < WI; ++i)
+                sa[i][w] = read_scale(scale_buffer, word + w, wr * 32 * WI + 32 * i + lm);
+#pragma unroll
+            for (int j = 0; j < WJ; ++j)
+                sb_new[j][w] = read_scale(scale_buffer, word + w, T::kRows + wc * 32 * WJ + 32 * j + lm);
+        }
+        // the second half of a half stage holds the first one's codes again: with scales of 2^-127 on both sides their products
+        // (below 2^-240) leave the fp32 sums as they are
+        if constexpr (last && !kE4M3) {
+            const uint32_t keep = half_stage ? 0u : ~0u;
+#pragma unroll
+            for (int i = 0; i < WI; ++i)
+                sa[i][kScaleWords - 1] &= keep;
+#pragma unroll
+            for (int j = 0; j < WJ; ++j)
+                sb_new[j][kScaleWords - 1] &= keep;
+        }
+        constexpr int kDmaSlots = 2 * kFragB;   // phases 1 and 2
+        auto phase = [&](auto blockc, auto numberc) __attribute__((always_inline)) {
+            constexpr int block = decltype(blockc)::value, number = decltype(numberc)::value;   // number: 0 = phase 1
+            constexpr bool before = number == 0;
+            constexpr bool from_zero = before ? (k & kAfterFirst) != 0 : (k & kStageFirst) != 0;
+            // the block whose output is stored meanwhile
+            constexpr int storing = boundary && number == 0 ? WI - 2 : boundary && number == 1 ? WI - 1
+                                    : last && number >= 2   ? block - 1
+                                                            : -1;
+            static_for<kFragB>([&](auto fc) {
+                constexpr int f = decltype(fc)::value;
+                multiply(blockc, fc, std::integral_constant<bool, from_zero>{}, before ? sa_before : sa[block]);
+                if constexpr (before)
+                    read_b(stage, fc);
+                // the next block's activations: four reads
+                constexpr int next = before ? 0 : block + 1;
+                static_for<4>([&](auto c) {
+                    if constexpr (decltype(c)::value * kFragB / 4 == f)
+                        read_a(stage, std::integral_constant<int, next>{}, c);
+                });
+                if constexpr (number < 2)
+                    static_for<kDma>([&](auto p) {
+                        if constexpr (decltype(p)::value * kDmaSlots / kDma == number * kFragB + f)
+                            transfer(p, refill, fetched, fetched_half);
+                    });
+                if constexpr (storing >= 0)
+                    static_for<kOutParts>([&](auto n) {
+                        if constexpr (decltype(n)::value * kFragB / kOutParts == f)
+                            store_part(std::integral_constant<int, storing>{}, n);
+                    });
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            if constexpr (before) {
+#pragma unroll
+                for (int j = 0; j < WJ; ++j)
+#pragma unroll
+                    for (int w = 0; w < kScaleWords; ++w)
+                        sb[j][w] = sb_new[j][w];
+            }
+        };
+        phase(std::integral_constant<int, WI - 1>{}, std::integral_constant<int, 0>{});
+        static_for<WI - 1>([&](auto i) { phase(i, std::integral_constant<int, decltype(i)::value + 1>{}); });
+        // the reads of block WI - 1 are back, the next stage has landed
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+        wait_vmcnt<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");        // no read of the new stage ahead of it
+        cur ^= 1;
+        scale_buffer ^= new_scales ? 1 : 0;
+    };
+    auto wave_part = [&]() {
+        out_m = m0 + wr * 32 * WI;
+        out_n = n0 + wc * 32 * WJ;
+    };
+
+    set_fetch_tile(tile, m0, n0);
+    next_m0 = m0;
+    next_n0 = n0;
+    transfer_scales(0, 0);
+    static_for<kDma>([&](auto p) { transfer(p, smem_addr, 0, false); });
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    // before the first tile: products of zeros, stored nowhere
+    out_m = M;
+    static_for<kFragB>([&](auto f) { bf[decltype(f)::value] = make_uint4(0, 0, 0, 0); });
+    static_for<4>([&](auto c) { af[0][decltype(c)::value] = af[1][decltype(c)::value] = make_uint4(0, 0, 0, 0); });
+    static_for<kScaleWords>([&](auto w) {
+        static_for<WI>([&](auto i) { sa[decltype(i)::value][decltype(w)::value] = 0; });
+        static_for<WJ>([&](auto j) { sb[decltype(j)::value][decltype(w)::value] = 0; });
+    });
+    static_for<WI>([&](auto i) { static_for<WJ>([&](auto j) { acc[decltype(i)::value][decltype(j)::value] = v16f{}; }); });
+    for (; tile < run_end; tile += peers) {
+        iteration(std::integral_constant<int, kStageFirst>{}, 0);
+        m0 = next_m0;
+        n0 = next_n0;
+        wave_part();
+        if constexpr (TWO) {
+            iteration(std::integral_constant<int, kAfterFirst | kStageLast>{}, 1);
+        } else {
+            iteration(std::integral_constant<int, kAfterFirst>{}, 1);
+            for (int at = 2; at < stages - 1; ++at)
+                iteration(std::integral_constant<int, 0>{}, at);
+            iteration(std::integral_constant<int, kStageLast>{}, stages - 1);
+        }
+    }
+    // the last block of the last tile
+    static_for<kFragB>([&](auto fc) { multiply(std::integral_constant<int, WI - 1>{}, fc, std::false_type{}, sa[WI - 1]); });
+    static_for<2>([&](auto b) {
+        static_for<kOutParts>([&](auto n) { store_part(std::integral_constant<int, WI - 2 + decltype(b)::value>{}, n); });
+    });
+}
+
+template <int FORMAT, int WI, int WJ>
+hipError_t launch_tiles(const MxGemmArgs &a, hipStream_t stream)
+{
+    typedef MxTile<FORMAT, WI, WJ> T;
+    const int tiles_m = (int)((a.M + T::kRows - 1) / T::kRows), tiles_n = (int)((a.N + T::kCols - 1) / T::kCols);
+    const int per_xcd = (int)(((int64_t)tiles_m * tiles_n + 7) / 8), peers = std::min(per_xcd, device_compute_units() / 8);
+    // (a tile's rows as one buffer: byte offsets below 2^31)
+    const bool pieces_fit = a.y && !a.acc_out && (a.ld_y & 7) == 0 && (a.N & 7) == 0 && a.ld_y < (1 << 24) &&
+                            (reinterpret_cast<uintptr_t>(a.y) & 15) == 0;
+    auto kernel = pieces_fit ? mx_tile_kernel<FORMAT, WI, WJ, false, false> : mx_tile_kernel<FORMAT, WI, WJ, false, true>;
+    if constexpr (!T::kE4M3) {   // (in E4M3 the shortest contraction has four)
+        if (a.K <= 2 * T::kStageK)
+            kernel = pieces_fit ? mx_tile_kernel<FORMAT, WI, WJ, true, false> : mx_tile_kernel<FORMAT, WI, WJ, true, true>;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(8 * peers)), dim3(kTileThreads), T::kLds, stream, a.a_codes, a.a_scales, a.b_codes,
+                       a.b_scales, (int)a.M, (int)a.N, (int)a.K, tiles_m, tiles_n, static_cast<uint16_t *>(a.y), a.ld_y, a.acc_out);
+    return hipGetLastError();
+}
+
+template <int FORMAT, int WI, int WJ, bool TWO>
+hipError_t prepare_tiles()
+{
+    constexpr int kLds = MxTile<FORMAT, WI, WJ>::kLds;
+    const hipError_t err = allow_dynamic_lds(reinterpret_cast<const void *>(mx_tile_kernel<FORMAT, WI, WJ, TWO, false>), kLds);
+    return err != hipSuccess ? err
+                             : allow_dynamic_lds(reinterpret_cast<const void *>(mx_tile_kernel<FORMAT, WI, WJ, TWO, true>), kLds);
+}
+
 template <int FORMAT>
 hipError_t launch_format(const MxGemmArgs &a, hipStream_t stream)
 {
+    if (a.M > 64 && a.K >= kScaleChunk && ((a.M + 255) / 256) * ((a.N + 255) / 256) >= 40)
+        return launch_tiles<FORMAT, 4, 4>(a, stream);
     return a.M <= 16 ? launch_few<FORMAT, 1, 1, 8>(a, stream) : launch_few<FORMAT, 4, 4, 4>(a, stream);
 }
 
@@ -156,6 +582,12 @@ hipError_t prepare_mx_gemm_kernels()
         hipError_t err = allow_dynamic_lds(reinterpret_cast<const void *>(mx_few_kernel<QUEST_MX_E2M1, 4, 4, 4>), 64 << 10);
         if (err == hipSuccess)
             err = allow_dynamic_lds(reinterpret_cast<const void *>(mx_few_kernel<QUEST_MX_E4M3, 4, 4, 4>), 64 << 10);
+        if (err == hipSuccess)
+            err = prepare_tiles<QUEST_MX_E2M1, 4, 4, false>();
+        if (err == hipSuccess)
+            err = prepare_tiles<QUEST_MX_E2M1, 4, 4, true>();
+        if (err == hipSuccess)
+            err = prepare_tiles<QUEST_MX_E4M3, 4, 4, false>();
         return err;
     });
 }

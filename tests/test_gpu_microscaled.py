@@ -210,6 +210,54 @@ def test_product(M, N, K, fmt):
     assert torch.equal(only_acc, acc)
 
 
+def sampled(count, rng):
+    """Ends, ends of tiles and others."""
+    at = {0, 31, 32, 127, 128, 255, 256, 257, count - 1, count - 2, count - 33} | set(rng.integers(0, count, 24).tolist())
+    return np.array(sorted(i for i in at if 0 <= i < count))
+
+
+@pytest.mark.parametrize("M,N,K", [(2100, 2200, 512), (2100, 2200, 640), (2303, 2056, 1152), (4097, 1288, 2048), (1800, 5128, 768)])
+@pytest.mark.parametrize("fmt", [E2M1, E4M3])
+def test_large_product(M, N, K, fmt):
+    """Sampled rows and columns by the bound, all outputs by their norm; the same bits whatever else is asked for."""
+    (ac, as_), (bc, bs) = random_operand(M, K, fmt, M), random_operand(N, K, E2M1, N + 1)
+    a, b = mx.values(ac, as_, fmt), mx.values(bc, bs, E2M1)
+    dev = on_device(ac, as_) + on_device(bc, bs)
+    y, acc = torch.full((M, N), float("nan"), dtype=BF16, device=DEV), torch.full((M, N), float("nan"), device=DEV)
+    q.quest_lowbit_gemm_mx(dev[0], dev[1], fmt, dev[2], dev[3], K, y=y)
+    q.quest_lowbit_gemm_mx(dev[0], dev[1], fmt, dev[2], dev[3], K, y=None, acc_out=acc)
+    assert torch.equal(y, acc.to(BF16))
+    rng = np.random.default_rng(K)
+    rows, cols = sampled(M, rng), sampled(N, rng)
+    ref = a[rows] @ b[cols].T
+    got = to_host_f64(acc[torch.from_numpy(rows).to(DEV)][:, torch.from_numpy(cols).to(DEV)])
+    assert np.all(np.abs(got - ref) <= product_bound(a[rows], b[cols], fmt) + 2.0 ** -24 * np.abs(ref))
+    whole = torch.from_numpy(a).to(DEV) @ torch.from_numpy(b).to(DEV).t()
+    # what the matrix instruction drops with E4M3 is below 2^-13 of a group's largest product: a few of 32 are that large
+    assert float((acc.double() - whole).norm()) <= (2.0 ** -20 if fmt == E2M1 else 2.0 ** -12) * float(whole.norm())
+    odd = torch.full((M, N + 3), -7.0, dtype=BF16, device=DEV)
+    q.quest_lowbit_gemm_mx(dev[0], dev[1], fmt, dev[2], dev[3], K, y=odd[:, :N])
+    assert torch.equal(odd[:, :N], y) and bool((odd[:, N:] == -7.0).all())
+
+
+@pytest.mark.parametrize("N", [2049, 2050, 2060])
+def test_large_product_of_columns_that_16_bytes_do_not_divide(N):
+    M, K = 2080, 640
+    (ac, as_), (bc, bs) = random_operand(M, K, E4M3, 1), random_operand(N, K, E2M1, 2)
+    dev = on_device(ac, as_) + on_device(bc, bs)
+    padded = on_device(*(np.concatenate([t, t[:(-N) % 8]]) for t in (bc, bs)))
+    ref = torch.empty(M, N + (-N) % 8, dtype=BF16, device=DEV)
+    q.quest_lowbit_gemm_mx(dev[0], dev[1], E4M3, *padded, K, y=ref)
+    for pitch in (0, 1, 8):
+        for start in (0, 1, 2):
+            flat = torch.full((start + M * (N + pitch) + 64,), -7.0, dtype=BF16, device=DEV)
+            y = flat[start:start + M * (N + pitch)].view(M, N + pitch)
+            q.quest_lowbit_gemm_mx(dev[0], dev[1], E4M3, dev[2], dev[3], K, y=y[:, :N])
+            assert torch.equal(y[:, :N], ref[:, :N])
+            assert bool((y[:, N:] == -7.0).all()) and bool((flat[:start] == -7.0).all())
+            assert bool((flat[start + M * (N + pitch):] == -7.0).all())
+
+
 @pytest.mark.parametrize("M,N,K", [(5, 70, 256), (300, 322, 256)])
 @pytest.mark.parametrize("pitch", [0, 1, 2, 6, 8])
 def test_product_into_wider_rows(M, N, K, pitch):
