@@ -158,8 +158,6 @@ hipError_t launch_few(const MxGemmArgs &a, hipStream_t stream)
 // workgroup's next tile, whose first products start from zero (C = 0, no accumulator is cleared), and block b of a finished
 // tile is rounded, parked in the wave's corner of LDS and stored as whole row segments while block b + 1 is multiplied.
 // ------------------------------------------------------------------------------------------
-typedef float v16f __attribute__((ext_vector_type(16)));
-
 constexpr int kTileThreads = 256;
 constexpr int kParkBytes = 32 * 128;       // 32 rows by 64 columns in bf16
 constexpr int kScaleChunk = 512;           // elements whose scales one transfer of 16 bytes per row brings
@@ -168,14 +166,31 @@ template <int FORMAT, int WI, int WJ>
 struct MxTile {
     static constexpr bool kE4M3 = FORMAT == QUEST_MX_E4M3;
     static constexpr int kRows = 64 * WI, kCols = 64 * WJ;
-    static constexpr int kSteps = kE4M3 ? 2 : 4;                 // matrix instructions along a stage (64 elements each)
-    static constexpr int kStageK = 64 * kSteps;
-    static constexpr int kRowA = 128, kRowB = 32 * kSteps;       // bytes of a row in a stage
+    static constexpr int kSteps = kE4M3 ? 1 : 2;                 // matrix instructions along a stage
+    static constexpr int kStageK = kUnit * kSteps;
+    static constexpr int kRowA = 128, kRowB = 64 * kSteps;       // bytes of a row in a stage
     static constexpr int kBytesA = kRows * kRowA, kStage = kBytesA + kCols * kRowB;
     static constexpr int kScales = (kRows + kCols) * 16;
     static constexpr int kLds = 2 * kStage + 2 * kScales + 4 * kParkBytes;
     static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
 };
+
+// a range of memory for buffer instructions, which leave out what lies beyond it
+__device__ __forceinline__ quest_v4u buffer_of(const void *p, uint32_t bytes)
+{
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    return quest_v4u{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, bytes, 0x00027000u};
+}
+
+// 16 bytes per lane from a buffer into LDS: lane l lands at lds_base + LDS_IMM + 16 l (see lds_dma16_at)
+template <int LDS_IMM>
+__device__ __forceinline__ void lds_buffer16_at(const quest_v4u &buffer, uint32_t lane_offset, uint32_t lds_base)
+{
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+                 :
+                 : "v"(lane_offset), "s"(buffer), "s"(lds_base), "n"(LDS_IMM)
+                 : "memory", "scc");
+}
 
 // what an iteration (a stage) of the stream is
 enum {
@@ -233,9 +248,8 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
 {
     typedef MxTile<FORMAT, WI, WJ> T;
     constexpr bool kE4M3 = T::kE4M3;
-    constexpr int SS = T::kSteps, kFragB = SS * WJ;      // weight fragments of a stage, matrix instructions of a phase
+    constexpr int NJ = 2 * WJ, kFragB = T::kSteps * NJ;  // 16-column fragments of a wave; of a whole stage
     constexpr int nA = 2 * WI, nB = T::kCols * T::kRowB / 4096, kDma = nA + nB;   // transfers of a wave and stage
-    constexpr int kScaleWords = SS / 2;                  // scale dwords of a row and stage
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
 
     // Tiles of this workgroup: each XCD (workgroup ids go to the eight in turn) has one contiguous run of tiles, ordered four
@@ -249,7 +263,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave >> 1, wc = wave & 1;
-    const int lm = lane & 31, lh = lane >> 5;
+    const int l16 = lane & 15, quarter = lane >> 4;
     const uint32_t smem_addr = lds_address(smem);
     const int64_t row_a = kE4M3 ? K : K / 2, row_b = K / 2;
     const int row_scales = K / 32;                       // bytes
@@ -257,100 +271,111 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
     const bool half_stage = K % T::kStageK != 0;         // E2M1: the last stage of a tile holds 128 elements
     const int words = K / 128;                           // scale dwords of a row
 
-    // ---- transfers, one stage ahead of the multiplication
-    uint32_t voff[kDma], scale_voff[2];
-    const uint8_t *fetch_a, *fetch_b, *fetch_as, *fetch_bs;   // the fetched tile's rows (wave-uniform)
+    // ---- transfers, one stage ahead of the multiplication.  One moves 1 KiB: lane l lands at 16 l, so it fetches the chunk that
+    // belongs there (see the reads below).  The rows of a tile are a buffer that ends with the operand: transfers of rows beyond
+    // it bring nothing that is used or stored.
+    quest_v4u fetch_a, fetch_b;
+    const uint8_t *fetch_as, *fetch_bs;
+    uint32_t fetch_rows_a, fetch_rows_b;
     auto set_fetch_tile = [&](int at, int &m0, int &n0) __attribute__((always_inline)) {
         const int band = at / (4 * tiles_n), band_rows = min(4, tiles_m - band * 4), in_band = at - band * 4 * tiles_n;
         m0 = __builtin_amdgcn_readfirstlane((band * 4 + in_band % band_rows) * T::kRows);
         n0 = __builtin_amdgcn_readfirstlane(in_band / band_rows * T::kCols);
-        const int last_a = M - 1 - m0, last_b = N - 1 - n0;   // rows beyond the edge: the last row again, not stored
-        fetch_a = a_codes + m0 * row_a;
-        fetch_b = b_codes + n0 * row_b;
+        fetch_rows_a = min(T::kRows, M - m0);
+        fetch_rows_b = min(T::kCols, N - n0);
+        fetch_a = buffer_of(a_codes + m0 * row_a, fetch_rows_a * (uint32_t)row_a);
+        fetch_b = buffer_of(b_codes + n0 * row_b, fetch_rows_b * (uint32_t)row_b);
         fetch_as = a_scales + (int64_t)m0 * row_scales;
         fetch_bs = b_scales + (int64_t)n0 * row_scales;
-        // a transfer moves 1 KiB: lane l lands at 16 l, so it fetches the chunk that belongs there (see the reads below)
-#pragma unroll
-        for (int p = 0; p < kDma; ++p) {
-            const bool left = p < nA;
-            const int piece = left ? wave * nA + p : wave * nB + p - nA;
-            if (left || T::kRowB == 128) {
-                const int row = piece * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
-                voff[p] = (uint32_t)min(row, left ? last_a : last_b) * (uint32_t)(left ? row_a : row_b) + 16u * chunk;
-            } else {
-                const int row = piece * 16 + (lane >> 2), chunk = (lane & 3) ^ ((row >> 2) & 3);
-                voff[p] = (uint32_t)min(row, last_b) * (uint32_t)row_b + 16u * chunk;
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int piece = wave + 4 * h;
-            scale_voff[h] = (uint32_t)(piece < WI ? min(64 * piece + lane, last_a) : min(64 * (piece - WI) + lane, last_b)) *
-                            (uint32_t)row_scales;
-        }
     };
-    // lanes whose chunk lies in the second half of a row's 128 bytes, which a half stage does not have: they fetch the first again
+    // Lanes' byte offsets, for rows of eight with an even and with an odd number, and what a half stage takes back of them: it
+    // has no second half of a row's 128 bytes, whose lanes fetch the first again.
+    uint32_t a_at[2], b_at[2];
     const uint32_t back[2] = {(lane & 4) ? 64u : 0u, (lane & 4) ? 0u : 64u};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int chunk = (lane & 7) ^ (4 * h + (lane >> 4));
+        a_at[h] = (uint32_t)(wave * nA * 8 + (lane >> 3)) * (uint32_t)row_a + 16u * chunk;
+        b_at[h] = T::kRowB == 128 ? (uint32_t)(wave * nB * 8 + (lane >> 3)) * (uint32_t)row_b + 16u * chunk
+                                  : (uint32_t)(wave * nB * 16 + (lane >> 2)) * (uint32_t)row_b + 16u * ((lane & 3) ^ (lane >> 4));
+    }
     auto transfer = [&](auto pc, uint32_t stage, int at, bool half) __attribute__((always_inline)) {
-        constexpr int p = decltype(pc)::value;
-        constexpr bool left = p < nA;
-        const uint32_t off = !kE4M3 && half ? voff[p] - back[p & 1] : voff[p];
-        if constexpr (left)
-            lds_dma16_at<1024 * p>(fetch_a + at * T::kRowA, off, stage + wave * (nA * 1024));
+        constexpr int p = decltype(pc)::value, h = p & 1, q = p - nA;
+        const uint32_t less = !kE4M3 && half ? back[h] : 0u;
+        if constexpr (p < nA)
+            lds_buffer16_at<1024 * p>(fetch_a, a_at[h] + (uint32_t)(8 * p * (int)row_a + at * T::kRowA) - less,
+                                      stage + wave * (nA * 1024));
         else
-            lds_dma16_at<T::kBytesA + 1024 * (p - nA)>(fetch_b + at * T::kRowB, off, stage + wave * (nB * 1024));
+            lds_buffer16_at<T::kBytesA + 1024 * q>(
+                fetch_b, b_at[h] + (uint32_t)((T::kRowB == 128 ? 8 : 16) * q * (int)row_b + at * T::kRowB) - less,
+                stage + wave * (nB * 1024));
     };
+    const uint32_t scale_at = (uint32_t)lane * (uint32_t)row_scales;
     const uint32_t scale_addr = smem_addr + 2 * T::kStage;
     // first scale dword of the 16 bytes that hold a stage's (the last ones of a row end where the row ends)
     auto chunk_start = [&](int at) { return min(at * T::kStageK / kScaleChunk * 4, words - 4); };
     auto transfer_scales = [&](int buffer, int at) __attribute__((always_inline)) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < (WI + WJ) / 4; ++h) {
             const int piece = wave + 4 * h;
-            if (piece < WI + WJ)
-                lds_dma16((piece < WI ? fetch_as : fetch_bs) + 4 * chunk_start(at), scale_voff[h],
-                          scale_addr + buffer * T::kScales + piece * 1024);
+            const bool left = piece < WI;
+            lds_buffer16_at<0>(buffer_of(left ? fetch_as : fetch_bs, (left ? fetch_rows_a : fetch_rows_b) * (uint32_t)row_scales),
+                               scale_at + (uint32_t)(64 * (left ? piece : piece - WI) * row_scales + 4 * chunk_start(at)),
+                               scale_addr + buffer * T::kScales + piece * 1024);
         }
     };
 
     // ---- fragments.  Chunk c of row r of 128 bytes sits at c ^ ((r >> 1) & 7) (64 bytes: c ^ ((r >> 2) & 3)): sixteen
     // consecutive rows then meet sixteen different 16-byte slots modulo 256 bytes.
-    //   E2M1, step ss: chunk 2 ss + lh;  E4M3: chunks 4 ss + lh and 4 ss + 2 + lh
-    uint4 af[2][4], bf[kFragB];            // activations: [block & 1][quarter of the 128 bytes]
-    uint32_t sa[WI][kScaleWords], sb[WJ][kScaleWords];
-    const uint32_t a_lane = (wr * 32 * WI + lm) * T::kRowA + ((lh ^ ((lm >> 1) & 7)) << 4);
-    const uint32_t b_lane = T::kBytesA + (wc * 32 * WJ + lm) * T::kRowB +
-                            ((T::kRowB == 128 ? lh ^ ((lm >> 1) & 7) : lh ^ ((lm >> 2) & 3)) << 4);
-    auto read_a = [&](const uint8_t *stage, auto block, auto quarter) __attribute__((always_inline)) {
-        constexpr int i = decltype(block)::value, c = decltype(quarter)::value;
-        af[i & 1][c] = *reinterpret_cast<const uint4 *>(stage + (a_lane ^ (c << 5)) + i * 32 * T::kRowA);
+    //   E2M1, step t: chunk 4 t + quarter;  E4M3: chunks quarter and 4 + quarter
+    uint4 af[2][2][2], bf[kFragB];         // activations: [block & 1][upper or lower 16 rows][chunk]
+    uint32_t sa[WI][2], sb[NJ];            // scale bytes of the lane's row: byte t for step t
+    const uint32_t a_lane = (wr * 32 * WI + l16) * T::kRowA + ((quarter ^ ((l16 >> 1) & 7)) << 4);
+    const uint32_t b_lane = T::kBytesA + (wc * 32 * WJ + l16) * T::kRowB +
+                            ((T::kRowB == 128 ? quarter ^ ((l16 >> 1) & 7) : quarter ^ ((l16 >> 2) & 3)) << 4);
+    auto read_a = [&](const uint8_t *stage, auto block, auto number) __attribute__((always_inline)) {
+        constexpr int i = decltype(block)::value, u = decltype(number)::value & 1, c = decltype(number)::value >> 1;
+        af[i & 1][u][c] = *reinterpret_cast<const uint4 *>(stage + (a_lane ^ (c << 6)) + (32 * i + 16 * u) * T::kRowA);
     };
     auto read_b = [&](const uint8_t *stage, auto frag) __attribute__((always_inline)) {
-        constexpr int f = decltype(frag)::value, ss = f / WJ, j = f % WJ;
-        bf[f] = *reinterpret_cast<const uint4 *>(stage + (b_lane ^ (ss << 5)) + j * 32 * T::kRowB);
+        constexpr int f = decltype(frag)::value, t = f / NJ, j = f % NJ;
+        bf[f] = *reinterpret_cast<const uint4 *>(stage + (b_lane ^ (t << 6)) + 16 * j * T::kRowB);
     };
-    // (shifted so that byte 0 is the lane's group of step 0, byte 2 that of step 1)
+    // A row's scales of a stage begin at dword `word` of its 16 bytes; the lane's byte is that of its quarter.  (E2M1: a pair that
+    // would begin at an odd dword belongs to a half stage, which has the first one only.)
+    const uint32_t pick = T::kSteps == 2 ? 0x0c0c0000u | (uint32_t)(4 + quarter) << 8 | (uint32_t)quarter : 0u;
     auto read_scale = [&](int buffer, int word, int row) __attribute__((always_inline)) {
-        return *reinterpret_cast<const uint32_t *>(smem + 2 * T::kStage + buffer * T::kScales + row * 16 + word * 4) >> (8 * lh);
+        const uint8_t *at = smem + 2 * T::kStage + buffer * T::kScales + row * 16;
+        if constexpr (T::kSteps == 2)
+            return *reinterpret_cast<const uint2 *>(at + (word & 2) * 4);
+        else
+            return *reinterpret_cast<const uint32_t *>(at + word * 4);
+    };
+    auto picked = [&](auto raw, int word) __attribute__((always_inline)) {
+        if constexpr (T::kSteps == 2)
+            return __builtin_amdgcn_perm(raw.y, (word & 1) ? raw.y : raw.x, pick);
+        else
+            return raw >> (8 * quarter);
     };
 
-    v16f acc[WI][WJ];
-    // matrix instruction f of block i: the weights are the row operand, so a lane's sums are four runs of consecutive outputs
-    auto multiply = [&](auto block, auto frag, auto from_zero, const uint32_t (&scale_a)[kScaleWords]) __attribute__((always_inline)) {
-        constexpr int i = decltype(block)::value, f = decltype(frag)::value, ss = f / WJ, j = f % WJ;
-        constexpr bool zero = decltype(from_zero)::value && ss == 0;
+    v4f acc[2 * WI][NJ];
+    // The two products of block i with weight fragment f: the weights are the row operand, so a lane's sums are four consecutive
+    // outputs of a row.  (Of the two forms of the instruction this one does more under the chip's power limit, from
+    // registers with random codes 6.5 against 6.0 PFLOP/s in E2M1 and 4.2 against 3.8 with E4M3: a sum is read and written
+    // once for 128 elements, not for 64.)
+    auto multiply = [&](auto block, auto frag, auto from_zero, const uint32_t (&scale_a)[2]) __attribute__((always_inline)) {
+        constexpr int i = decltype(block)::value, f = decltype(frag)::value, t = f / NJ, j = f % NJ;
+        constexpr bool zero = decltype(from_zero)::value && t == 0;
         const v8i b = v8i{(int)bf[f].x, (int)bf[f].y, (int)bf[f].z, (int)bf[f].w, 0, 0, 0, 0};
-        v8i a;
-        if constexpr (kE4M3) {
-            const uint4 &lo = af[i & 1][2 * ss], &hi = af[i & 1][2 * ss + 1];
-            a = v8i{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-        } else {
-            const uint4 &lo = af[i & 1][ss];
-            a = v8i{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, 0, 0, 0, 0};
-        }
-        const v16f c = zero ? v16f{} : acc[i][j];
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, c, kF4, kE4M3 ? kF8 : kF4, 2 * (ss & 1),
-                                                                    (int)sb[j][ss / 2], 2 * (ss & 1), (int)scale_a[ss / 2]);
+        static_for<2>([&](auto uc) {
+            constexpr int u = decltype(uc)::value;
+            const uint4 &lo = af[i & 1][u][kE4M3 ? 0 : t], &hi = af[i & 1][u][1];
+            const v8i a = kE4M3 ? v8i{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w}
+                                : v8i{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, 0, 0, 0, 0};
+            v4f &sum = acc[2 * i + u][j];
+            sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, zero ? v4f{0, 0, 0, 0} : sum, kF4, kE4M3 ? kF8 : kF4, t,
+                                                                   (int)sb[j], t, (int)scale_a[u]);
+        });
     };
 
     // ---- the output of a finished tile
@@ -364,24 +389,23 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
         constexpr int i = decltype(block)::value, piece = decltype(part)::value / 6, n = decltype(part)::value % 6;
         if constexpr (GENERAL && n == 0 && piece == 0) {
             if (acc_out)
-                static_for<WJ>([&](auto jc) {
-                    constexpr int j = decltype(jc)::value;
+                static_for<2 * NJ>([&](auto tc) {
+                    constexpr int u = decltype(tc)::value / NJ, j = decltype(tc)::value % NJ;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int m = out_m + 32 * i + lm, col = out_n + 32 * j + 8 * (r >> 2) + 4 * lh + (r & 3);
+                    for (int e = 0; e < 4; ++e) {
+                        const int m = out_m + 32 * i + 16 * u + l16, col = out_n + 16 * j + 4 * quarter + e;
                         if (m < M && col < N)
-                            acc_out[(int64_t)m * N + col] = acc[i][j][r];
+                            acc_out[(int64_t)m * N + col] = acc[2 * i + u][j][e];
                     }
                 });
         }
         if constexpr (n < 4) {             // columns 16 n .. + 16 of the piece
-            constexpr int j = 2 * piece + n / 2;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int g = 2 * (n & 1) + h;
-                *reinterpret_cast<uint2 *>(park + lm * 128 + (((4 * (n / 2) + g) ^ (lm & 7)) << 4) + 8 * lh) =
-                    make_uint2(pack_bf16(acc[i][j][4 * g], acc[i][j][4 * g + 1]), pack_bf16(acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]));
-            }
+            static_for<2>([&](auto uc) {
+                constexpr int u = decltype(uc)::value;
+                const v4f &sum = acc[2 * i + u][4 * piece + n];
+                *reinterpret_cast<uint2 *>(park + (16 * u + l16) * 128 + (((2 * n + (quarter >> 1)) ^ (l16 & 7)) << 4) + 8 * (quarter & 1)) =
+                    make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
+            });
         } else if constexpr (GENERAL) {
             if (n == 5 && y && out_m + 32 * i < M && out_n + 64 * piece < N)
                 store_ragged_piece(park, y, ld_y, out_m + 32 * i, out_n + 64 * piece, M, N, lane);
@@ -420,30 +444,30 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
         const bool new_scales = fetched * T::kStageK % kScaleChunk == 0;
         if (new_scales)
             transfer_scales(scale_buffer ^ 1, fetched);
-        // this stage's scales; those of the block that phase 1 finishes stay until then
-        uint32_t sa_before[kScaleWords], sb_new[WJ][kScaleWords];
-        const int word = at * (T::kStageK / 128) - chunk_start(at);
-#pragma unroll
-        for (int w = 0; w < kScaleWords; ++w) {
-            sa_before[w] = sa[WI - 1][w];
-#pragma unroll
-            for (int i = 0; i < WI; ++i)
-                sa[i][w] = read_scale(scale_buffer, word + w, wr * 32 * WI + 32 * i + lm);
-#pragma unroll
-            for (int j = 0; j < WJ; ++j)
-                sb_new[j][w] = read_scale(scale_buffer, word + w, T::kRows + wc * 32 * WJ + 32 * j + lm);
-        }
+        // This stage's scales: read during phase 1, whose products need those of the stage before
+        uint32_t sb_new[NJ];
+        const uint32_t sa_before[2] = {sa[WI - 1][0], sa[WI - 1][1]};
+        const int word = at * T::kSteps - chunk_start(at);
+        constexpr int kRowScales = 2 * WI + NJ, kPerSlot = (kRowScales + kFragB - 1) / kFragB, kBehind = 4 / kPerSlot;
+        decltype(read_scale(0, 0, 0)) raw[kRowScales];
         // the second half of a half stage holds the first one's codes again: with scales of 2^-127 on both sides their products
         // (below 2^-240) leave the fp32 sums as they are
-        if constexpr (last && !kE4M3) {
-            const uint32_t keep = half_stage ? 0u : ~0u;
-#pragma unroll
-            for (int i = 0; i < WI; ++i)
-                sa[i][kScaleWords - 1] &= keep;
-#pragma unroll
-            for (int j = 0; j < WJ; ++j)
-                sb_new[j][kScaleWords - 1] &= keep;
-        }
+        const uint32_t keep = last && !kE4M3 && half_stage ? 0xffu : ~0u;
+        auto scale_slot = [&](auto slot) __attribute__((always_inline)) {
+            static_for<kPerSlot>([&](auto more) {
+                constexpr int now = decltype(slot)::value * kPerSlot + decltype(more)::value, then = now - kBehind * kPerSlot;
+                if constexpr (now < kRowScales)
+                    raw[now] = read_scale(scale_buffer, word, now < 2 * WI ? wr * 32 * WI + 16 * now + l16
+                                                                           : T::kRows + wc * 32 * WJ + 16 * (now - 2 * WI) + l16);
+                if constexpr (then >= 0 && then < kRowScales) {
+                    const uint32_t scale = last && !kE4M3 ? picked(raw[then], word) & keep : picked(raw[then], word);
+                    if constexpr (then < 2 * WI)
+                        sa[then / 2][then % 2] = scale;
+                    else
+                        sb_new[then - 2 * WI] = scale;
+                }
+            });
+        };
         constexpr int kDmaSlots = 2 * kFragB;   // phases 1 and 2
         auto phase = [&](auto blockc, auto numberc) __attribute__((always_inline)) {
             constexpr int block = decltype(blockc)::value, number = decltype(numberc)::value;   // number: 0 = phase 1
@@ -458,10 +482,12 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
                 multiply(blockc, fc, std::integral_constant<bool, from_zero>{}, before ? sa_before : sa[block]);
                 if constexpr (before)
                     read_b(stage, fc);
-                // the next block's activations: four reads
+                if constexpr (before)
+                    scale_slot(fc);
+                // the next block's activations: four reads, as early as their registers are free
                 constexpr int next = before ? 0 : block + 1;
                 static_for<4>([&](auto c) {
-                    if constexpr (decltype(c)::value * kFragB / 4 == f)
+                    if constexpr (decltype(c)::value / 2 == f)
                         read_a(stage, std::integral_constant<int, next>{}, c);
                 });
                 if constexpr (number < 2)
@@ -477,11 +503,10 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
                 __builtin_amdgcn_sched_barrier(0);
             });
             if constexpr (before) {
+                static_for<kBehind>([&](auto more) { scale_slot(std::integral_constant<int, kFragB + decltype(more)::value>{}); });
 #pragma unroll
-                for (int j = 0; j < WJ; ++j)
-#pragma unroll
-                    for (int w = 0; w < kScaleWords; ++w)
-                        sb[j][w] = sb_new[j][w];
+                for (int j = 0; j < NJ; ++j)
+                    sb[j] = sb_new[j];
             }
         };
         phase(std::integral_constant<int, WI - 1>{}, std::integral_constant<int, 0>{});
@@ -510,12 +535,13 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
     // before the first tile: products of zeros, stored nowhere
     out_m = M;
     static_for<kFragB>([&](auto f) { bf[decltype(f)::value] = make_uint4(0, 0, 0, 0); });
-    static_for<4>([&](auto c) { af[0][decltype(c)::value] = af[1][decltype(c)::value] = make_uint4(0, 0, 0, 0); });
-    static_for<kScaleWords>([&](auto w) {
-        static_for<WI>([&](auto i) { sa[decltype(i)::value][decltype(w)::value] = 0; });
-        static_for<WJ>([&](auto j) { sb[decltype(j)::value][decltype(w)::value] = 0; });
+    static_for<4>([&](auto c) {
+        constexpr int u = decltype(c)::value & 1, h = decltype(c)::value >> 1;
+        af[0][u][h] = af[1][u][h] = make_uint4(0, 0, 0, 0);
     });
-    static_for<WI>([&](auto i) { static_for<WJ>([&](auto j) { acc[decltype(i)::value][decltype(j)::value] = v16f{}; }); });
+    static_for<WI>([&](auto i) { sa[decltype(i)::value][0] = sa[decltype(i)::value][1] = 0; });
+    static_for<NJ>([&](auto j) { sb[decltype(j)::value] = 0; });
+    static_for<2 * WI>([&](auto i) { static_for<NJ>([&](auto j) { acc[decltype(i)::value][decltype(j)::value] = v4f{0, 0, 0, 0}; }); });
     for (; tile < run_end; tile += peers) {
         iteration(std::integral_constant<int, kStageFirst>{}, 0);
         m0 = next_m0;
