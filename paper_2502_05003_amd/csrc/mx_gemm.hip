@@ -153,7 +153,7 @@ hipError_t launch_few(const MxGemmArgs &a, hipStream_t stream)
 //   barrier: the stage has landed, the other buffer has been left by all waves
 //   phase 1   multiply block WI - 1 of the stage before; each weight fragment that is done with is replaced by the new stage's
 //   phase 2   block 0 of the stage;  phase 3 ..  blocks 1 .. WI - 2
-//   wait for the reads of block WI - 1 and for the next stage's transfers, which phases 1 and 2 have issued; barrier
+//   wait for the reads of block WI - 1 and for the next stage's transfers, which the first phases have issued; barrier
 // Nothing but the waits for these two interrupts the matrix instructions, tile ends included: the transfers run on into the
 // workgroup's next tile, whose first products start from zero (C = 0, no accumulator is cleared), and block b of a finished
 // tile is rounded, parked in the wave's corner of LDS and stored as whole row segments while block b + 1 is multiplied.
@@ -190,6 +190,14 @@ __device__ __forceinline__ void lds_buffer16_at(const quest_v4u &buffer, uint32_
                  :
                  : "v"(lane_offset), "s"(buffer), "s"(lds_base), "n"(LDS_IMM)
                  : "memory", "scc");
+}
+
+// The same IMM bytes further on in the buffer and in LDS, with M0 as it was left
+template <int IMM>
+__device__ __forceinline__ void lds_buffer16_next(const quest_v4u &buffer, uint32_t lane_offset)
+{
+    static_assert(IMM >= 0 && IMM < 4096, "the instruction's offset field");
+    asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" : : "v"(lane_offset), "s"(buffer), "n"(IMM) : "memory");
 }
 
 // what an iteration (a stage) of the stream is
@@ -302,13 +310,23 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
     auto transfer = [&](auto pc, uint32_t stage, int at, bool half) __attribute__((always_inline)) {
         constexpr int p = decltype(pc)::value, h = p & 1, q = p - nA;
         const uint32_t less = !kE4M3 && half ? back[h] : 0u;
-        if constexpr (p < nA)
-            lds_buffer16_at<1024 * p>(fetch_a, a_at[h] + (uint32_t)(8 * p * (int)row_a + at * T::kRowA) - less,
-                                      stage + wave * (nA * 1024));
-        else
-            lds_buffer16_at<T::kBytesA + 1024 * q>(
-                fetch_b, b_at[h] + (uint32_t)((T::kRowB == 128 ? 8 : 16) * q * (int)row_b + at * T::kRowB) - less,
-                stage + wave * (nB * 1024));
+        // (M0 for four at a time: the others differ in the instruction's offset, which moves both ends; rows are 256 bytes or more
+        // apart, so the offset in memory that makes up for it is not negative)
+        if constexpr (p < nA) {
+            constexpr int more = 1024 * (p % 4);
+            const uint32_t from = a_at[h] + (uint32_t)(8 * p * (int)row_a + at * T::kRowA - more) - less;
+            if constexpr (more == 0)
+                lds_buffer16_at<1024 * p>(fetch_a, from, stage + wave * (nA * 1024));
+            else
+                lds_buffer16_next<more>(fetch_a, from);
+        } else {
+            constexpr int more = 1024 * (q % 4);
+            const uint32_t from = b_at[h] + (uint32_t)((T::kRowB == 128 ? 8 : 16) * q * (int)row_b + at * T::kRowB - more) - less;
+            if constexpr (more == 0)
+                lds_buffer16_at<T::kBytesA + 1024 * q>(fetch_b, from, stage + wave * (nB * 1024));
+            else
+                lds_buffer16_next<more>(fetch_b, from);
+        }
     };
     const uint32_t scale_at = (uint32_t)lane * (uint32_t)row_scales;
     const uint32_t scale_addr = smem_addr + 2 * T::kStage;
@@ -343,7 +361,8 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
     };
     // A row's scales of a stage begin at dword `word` of its 16 bytes; the lane's byte is that of its quarter.  (E2M1: a pair that
     // would begin at an odd dword belongs to a half stage, which has the first one only.)
-    const uint32_t pick = T::kSteps == 2 ? 0x0c0c0000u | (uint32_t)(4 + quarter) << 8 | (uint32_t)quarter : 0u;
+    const uint32_t pick_pair = 0x0c0c0000u | (uint32_t)(4 + quarter) << 8 | (uint32_t)quarter;
+    const uint32_t pick_first = 0x0c0c0c00u | (uint32_t)quarter, pick_second = 0x0c0c0c04u + (uint32_t)quarter;
     auto read_scale = [&](int buffer, int word, int row) __attribute__((always_inline)) {
         const uint8_t *at = smem + 2 * T::kStage + buffer * T::kScales + row * 16;
         if constexpr (T::kSteps == 2)
@@ -351,11 +370,11 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
         else
             return *reinterpret_cast<const uint32_t *>(at + word * 4);
     };
-    auto picked = [&](auto raw, int word) __attribute__((always_inline)) {
+    auto picked = [&](auto raw, uint32_t by) __attribute__((always_inline)) {
         if constexpr (T::kSteps == 2)
-            return __builtin_amdgcn_perm(raw.y, (word & 1) ? raw.y : raw.x, pick);
+            return __builtin_amdgcn_perm(raw.y, raw.x, by);
         else
-            return raw >> (8 * quarter);
+            return raw >> by;
     };
 
     v4f acc[2 * WI][NJ];
@@ -450,9 +469,11 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
         const int word = at * T::kSteps - chunk_start(at);
         constexpr int kRowScales = 2 * WI + NJ, kPerSlot = (kRowScales + kFragB - 1) / kFragB, kBehind = 4 / kPerSlot;
         decltype(read_scale(0, 0, 0)) raw[kRowScales];
-        // the second half of a half stage holds the first one's codes again: with scales of 2^-127 on both sides their products
-        // (below 2^-240) leave the fp32 sums as they are
-        const uint32_t keep = last && !kE4M3 && half_stage ? 0xffu : ~0u;
+        // The second half of a half stage holds the first one's codes again: with scales of 2^-127 on both sides their products
+        // (below 2^-240) leave the fp32 sums as they are.
+        uint32_t pick = T::kSteps == 2 ? pick_pair : 8u * quarter;
+        if constexpr (last && !kE4M3)
+            pick = !half_stage ? pick : (word & 1) ? pick_second : pick_first;
         auto scale_slot = [&](auto slot) __attribute__((always_inline)) {
             static_for<kPerSlot>([&](auto more) {
                 constexpr int now = decltype(slot)::value * kPerSlot + decltype(more)::value, then = now - kBehind * kPerSlot;
@@ -460,15 +481,15 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
                     raw[now] = read_scale(scale_buffer, word, now < 2 * WI ? wr * 32 * WI + 16 * now + l16
                                                                            : T::kRows + wc * 32 * WJ + 16 * (now - 2 * WI) + l16);
                 if constexpr (then >= 0 && then < kRowScales) {
-                    const uint32_t scale = last && !kE4M3 ? picked(raw[then], word) & keep : picked(raw[then], word);
                     if constexpr (then < 2 * WI)
-                        sa[then / 2][then % 2] = scale;
+                        sa[then / 2][then % 2] = picked(raw[then], pick);
                     else
-                        sb_new[then - 2 * WI] = scale;
+                        sb_new[then - 2 * WI] = picked(raw[then], pick);
                 }
             });
         };
-        constexpr int kDmaSlots = 2 * kFragB;   // phases 1 and 2
+        // transfers spread over phases 1 and 2, in E2M1, which has more of them, over 3 (4096 x 4096 x 16640: 143 -> 139 us)
+        constexpr int kDmaPhases = kE4M3 || WI < 4 ? 2 : 3, kDmaSlots = kDmaPhases * kFragB;
         auto phase = [&](auto blockc, auto numberc) __attribute__((always_inline)) {
             constexpr int block = decltype(blockc)::value, number = decltype(numberc)::value;   // number: 0 = phase 1
             constexpr bool before = number == 0;
@@ -490,7 +511,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
                     if constexpr (decltype(c)::value / 2 == f)
                         read_a(stage, std::integral_constant<int, next>{}, c);
                 });
-                if constexpr (number < 2)
+                if constexpr (number < kDmaPhases)
                     static_for<kDma>([&](auto p) {
                         if constexpr (decltype(p)::value * kDmaSlots / kDma == number * kFragB + f)
                             transfer(p, refill, fetched, fetched_half);
