@@ -10,6 +10,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 
+template <int WAVES>
 __device__ __forceinline__ float block_sum(float v, float *park)
 {
     v = wave_sum_dpp(v);
@@ -19,9 +20,16 @@ __device__ __forceinline__ float block_sum(float v, float *park)
     __syncthreads();
     float sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
+    for (int w = 0; w < WAVES; ++w)
         sum += park[w];
     return sum;
+}
+
+// eight elements rounded to the type (bf16: by the hardware's conversion)
+__device__ __forceinline__ void store8_packed(float *p, const float (&v)[8]) { store8(p, v); }
+__device__ __forceinline__ void store8_packed(uint16_t *p, const float (&v)[8])
+{
+    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
 // rounded to the type and back
@@ -55,13 +63,13 @@ __global__ __launch_bounds__(kThreads) void rms_norm_kernel(const T *__restrict_
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 v[i][e] = rounded(v[i][e] + r[e], x);
-            store8(h_out + first + c, v[i]);
+            store8_packed(h_out + first + c, v[i]);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             sum = __fmaf_rn(v[i][e], v[i][e], sum);
     }
-    const float mean = block_sum(sum, park) / (float)cols + eps;
+    const float mean = block_sum<kWaves>(sum, park) / (float)cols + eps;
     const float rstd = mean == 0.0f ? 0.0f : mean < INFINITY ? 1.0f / sqrtf(mean) : NAN;
     if (rstd_out && threadIdx.x == 0)
         rstd_out[row] = rstd;
@@ -75,7 +83,7 @@ __global__ __launch_bounds__(kThreads) void rms_norm_kernel(const T *__restrict_
             for (int e = 0; e < 8; ++e)
                 v[i][e] = __fmul_rn(__fmul_rn(v[i][e], rstd), w[e]);
             if (y_out)
-                store8(y_out + first + c, v[i]);
+                store8_packed(y_out + first + c, v[i]);
         }
         if (codes) {
             wave_hadamard(v[i], log2n, norm, lane);
@@ -95,82 +103,184 @@ __global__ __launch_bounds__(kThreads) void rms_norm_kernel(const T *__restrict_
     }
 }
 
-// A workgroup takes the rows blockIdx.x, + gridDim.x, ..; its share of dweight stays in registers until it is done.
-template <typename T, typename W, int CH>
-__global__ __launch_bounds__(kThreads) void rms_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ h,
+/*
+ * Backward pass.  Bound by memory: h, dy and dh are read and dx is written once (16384 x 2048 in bf16 268 MB, 52 us at the 5.1 TB/s
+ * of a large copy).  A row belongs to GROUP waves, CH chunks of eight elements to a lane; a group takes every (number of
+ * groups)-th row, with the next row's loads in flight while it works on one, and keeps its share of dweight in registers.  One wave
+ * to a row up to 2048 elements: no barrier then ties waves together.  The groups of a workgroup add up their shares
+ * in LDS; the workgroups' go to the workspace, where rms_norm_dweight_kernel adds them in a fixed order.
+ * (us, with a workgroup to a row, one row at a time and dweight's sum in a workgroup per 256 columns / so: 16384 x 2048 in bf16
+ * 185 / 55; 777 x 640 in fp32 116 / 14, of which the call itself is most)
+ */
+template <typename T, int CH>
+struct RowLoads {   // as they come from memory
+    static constexpr int kQuads = CH * 8 * (int)sizeof(T) / 16;
+    uint4 h[kQuads], dy[kQuads], dh[kQuads];
+    float rstd;
+};
+
+__device__ __forceinline__ void widened(const uint4 *raw, float (&v)[8], const float *)
+{
+    const float4 a = __builtin_bit_cast(float4, raw[0]), b = __builtin_bit_cast(float4, raw[1]);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void widened(const uint4 *raw, float (&v)[8], const uint16_t *)
+{
+    const uint4 w = raw[0];
+    v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u);
+    v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
+    v[4] = __uint_as_float(w.z << 16); v[5] = __uint_as_float(w.z & 0xffff0000u);
+    v[6] = __uint_as_float(w.w << 16); v[7] = __uint_as_float(w.w & 0xffff0000u);
+}
+
+// threads of a workgroup: four rows of a wave each, or one row of GROUP waves
+constexpr int backward_threads(int group)
+{
+    return group == 1 ? kThreads : kWave * group;
+}
+
+template <typename T, typename W, int GROUP, int CH, bool ALONG>
+__global__ __launch_bounds__(backward_threads(GROUP)) void rms_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ h,
                                                                      const W *__restrict__ weight, const float *__restrict__ rstd_in,
                                                                      const T *__restrict__ dh, int64_t rows, int cols,
                                                                      T *__restrict__ dx, float *__restrict__ partial)
 {
-    __shared__ float park[kWaves];
-    float dw[CH][8] = {};
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+    constexpr int kBlock = backward_threads(GROUP), kGroupThreads = kWave * GROUP, kGroups = kBlock / kGroupThreads;
+    constexpr bool kAhead = CH * sizeof(T) <= 8;      // (else the next row's loads would not fit the registers)
+    constexpr int kQuads = 8 * (int)sizeof(T) / 16;   // of a chunk
+    extern __shared__ float shares[];                 // [groups][cols], where dweight is wanted
+    __shared__ float park[GROUP];
+    const int group = threadIdx.x / kGroupThreads, t = threadIdx.x % kGroupThreads;
+    float dw[CH][8] = {}, w[CH][8];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int c = (i * kGroupThreads + t) * 8;
+        if (c < cols)
+            load8(weight + c, w[i]);
+    }
+    typedef RowLoads<T, CH> Loads;
+    auto fetch = [&](Loads &l, int64_t row) {
         const int64_t first = row * cols;
-        const float rstd = rstd_in[row];
-        float xhat[CH][8], t[CH][8], sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int c = (i * kThreads + threadIdx.x) * 8;
+            const int c = (i * kGroupThreads + t) * 8;
             if (c >= cols)
                 continue;
-            float g[8], w[8];
-            load8(h + first + c, xhat[i]);
-            load8(dy + first + c, g);
-            load8(weight + c, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                xhat[i][e] *= rstd;
-                dw[i][e] = __fmaf_rn(g[e], xhat[i][e], dw[i][e]);
-                t[i][e] = g[e] * w[e];
-                sum = __fmaf_rn(t[i][e], xhat[i][e], sum);
+            for (int k = 0; k < kQuads; ++k) {
+                l.h[i * kQuads + k] = reinterpret_cast<const uint4 *>(h + first + c)[k];
+                l.dy[i * kQuads + k] = reinterpret_cast<const uint4 *>(dy + first + c)[k];
+                if constexpr (ALONG)
+                    l.dh[i * kQuads + k] = reinterpret_cast<const uint4 *>(dh + first + c)[k];
             }
         }
-        const float mean = block_sum(sum, park) / (float)cols;
+        l.rstd = rstd_in[row];
+    };
+    // (the same number of rounds for every group of a workgroup: they meet at barriers)
+    const int64_t stride = (int64_t)gridDim.x * kGroups;
+    int64_t row = (int64_t)blockIdx.x * kGroups + group;
+    Loads next;
+    if (kAhead && row < rows)
+        fetch(next, row);
+    for (int64_t round = (int64_t)blockIdx.x * kGroups; round < rows; round += stride, row += stride) {
+        const bool mine = row < rows;
+        if (!kAhead && mine)
+            fetch(next, row);
+        const Loads now = next;
+        if (kAhead && row + stride < rows)
+            fetch(next, row + stride);
+        float xhat[CH][8], g[CH][8], sum = 0.0f;
+        if (mine) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const int c = (i * kThreads + threadIdx.x) * 8;
-            if (c >= cols)
-                continue;
-            float r[8];
-            if (dh) {
-                load8(dh + first + c, r);
-            } else {
+            for (int i = 0; i < CH; ++i) {
+                if ((i * kGroupThreads + t) * 8 >= cols)
+                    continue;
+                widened(now.h + i * kQuads, xhat[i], h);
+                widened(now.dy + i * kQuads, g[i], h);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    xhat[i][e] *= now.rstd;
+                    dw[i][e] = __fmaf_rn(g[i][e], xhat[i][e], dw[i][e]);
+                    g[i][e] *= w[i][e];
+                    sum = __fmaf_rn(g[i][e], xhat[i][e], sum);
+                }
+            }
+        }
+        const float mean = (GROUP == 1 ? wave_sum_dpp(sum) : block_sum<GROUP>(sum, park)) / (float)cols;
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int c = (i * kGroupThreads + t) * 8;
+                if (c >= cols)
+                    continue;
+                float r[8] = {};
+                if constexpr (ALONG)
+                    widened(now.dh + i * kQuads, r, h);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    r[e] = 0.0f;
+                    r[e] = __fmaf_rn(now.rstd, __fmaf_rn(-xhat[i][e], mean, g[i][e]), r[e]);
+                store8_packed(dx + row * cols + c, r);
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                r[e] = __fmaf_rn(rstd, __fmaf_rn(-xhat[i][e], mean, t[i][e]), r[e]);
-            store8(dx + first + c, r);
         }
     }
     if (!partial)
         return;
+    float *const mine = partial + (int64_t)blockIdx.x * cols;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = (i * kThreads + threadIdx.x) * 8;
+        const int c = (i * kGroupThreads + t) * 8;
         if (c < cols)
-            store8(partial + (int64_t)blockIdx.x * cols + c, dw[i]);
+            store8(kGroups == 1 ? mine + c : shares + group * cols + c, dw[i]);
+    }
+    if constexpr (kGroups > 1) {
+        __syncthreads();
+        for (int c = threadIdx.x * 4; c < cols; c += kBlock * 4) {
+            float4 sum = *reinterpret_cast<const float4 *>(shares + c);
+#pragma unroll
+            for (int o = 1; o < kGroups; ++o) {
+                const float4 v = *reinterpret_cast<const float4 *>(shares + o * cols + c);
+                sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+            }
+            *reinterpret_cast<float4 *>(mine + c) = sum;
+        }
     }
 }
 
-// dweight[j] = the sum of `parts` partial rows, in their order
-__global__ __launch_bounds__(kThreads) void rms_norm_dweight_kernel(const float *__restrict__ partial, int parts, int cols,
-                                                                    float *__restrict__ dweight)
+// dweight[j] = the sum of `parts` partial rows: 64 columns to a workgroup, its waves take the rows in turn and meet in LDS
+constexpr int kSumWaves = 16;
+__global__ __launch_bounds__(kWave *kSumWaves) void rms_norm_dweight_kernel(const float *__restrict__ partial, int parts, int cols,
+                                                                            float *__restrict__ dweight)
 {
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= cols)
-        return;
+    __shared__ float sums[kSumWaves][kWave];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * kWave + lane;
     float sum = 0.0f;
-    for (int p = 0; p < parts; ++p)
-        sum += partial[(int64_t)p * cols + c];
-    dweight[c] = sum;
+    if (c < cols) {
+#pragma unroll 8
+        for (int p = wave; p < parts; p += kSumWaves)
+            sum += partial[(int64_t)p * cols + c];
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && c < cols) {
+#pragma unroll
+        for (int o = 1; o < kSumWaves; ++o)
+            sum += sums[o][lane];
+        dweight[c] = sum;
+    }
 }
 
-int parts_of(int64_t rows)
+constexpr int64_t kOneWave = 2048;   // row length up to which a wave has a row to itself in the backward pass
+
+int groups_of(int64_t cols)
 {
-    return (int)std::min<int64_t>(rows, 512);
+    return cols <= kOneWave ? kWaves : 1;
+}
+
+// workgroups of the backward pass where dweight is wanted, each with a partial row: two for each compute unit, no more than rows need
+int parts_of(int64_t rows, int64_t cols)
+{
+    return (int)std::min<int64_t>((rows + groups_of(cols) - 1) / groups_of(cols), 512);
 }
 
 // f(std::integral_constant<int, CH>) for the number of chunks of 2048 elements that a row has
@@ -204,21 +314,34 @@ hipError_t launch_forward(const RmsNormArgs &a, hipStream_t stream)
 template <typename T, typename W>
 hipError_t launch_backward(const RmsNormBackwardArgs &a, hipStream_t stream)
 {
-    const int parts = parts_of(a.rows);
+    const int parts = parts_of(a.rows, a.cols), groups = groups_of(a.cols);
     float *partial = a.dweight ? static_cast<float *>(a.workspace) : nullptr;
     hipError_t err = hipSuccess;
     if (a.rows > 0) {
-        // (without dweight nothing ties rows to a workgroup)
-        const unsigned blocks = partial ? (unsigned)parts : (unsigned)std::min<int64_t>(a.rows, 1 << 20);
-        with_chunks(a.cols, [&](auto ch) {
-            hipLaunchKernelGGL((rms_norm_backward_kernel<T, W, decltype(ch)::value>), dim3(blocks), dim3(kThreads), 0, stream,
+        auto launch = [&](auto group, auto ch) {
+            constexpr int G = decltype(group)::value, CH = decltype(ch)::value;
+            auto kernel = a.dh ? rms_norm_backward_kernel<T, W, G, CH, true> : rms_norm_backward_kernel<T, W, G, CH, false>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)parts), dim3(backward_threads(G)), groups > 1 ? groups * a.cols * sizeof(float) : 0, stream,
                                static_cast<const T *>(a.dy), static_cast<const T *>(a.h), static_cast<const W *>(a.weight), a.rstd,
                                static_cast<const T *>(a.dh), a.rows, (int)a.cols, static_cast<T *>(a.dx), partial);
-        });
+        };
+        typedef std::integral_constant<int, 1> One;
+        if (a.cols <= 512)
+            launch(One(), One());
+        else if (a.cols <= 1024)
+            launch(One(), std::integral_constant<int, 2>());
+        else if (a.cols <= kOneWave)
+            launch(One(), std::integral_constant<int, 4>());
+        else if (a.cols <= 4096)
+            launch(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
+        else if (a.cols <= 8192)
+            launch(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
+        else
+            launch(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
         err = hipGetLastError();
     }
     if (err == hipSuccess && a.dweight) {
-        hipLaunchKernelGGL(rms_norm_dweight_kernel, dim3((unsigned)((a.cols + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream,
+        hipLaunchKernelGGL(rms_norm_dweight_kernel, dim3((unsigned)((a.cols + kWave - 1) / kWave)), dim3(kWave * kSumWaves), 0, stream,
                            partial, parts, (int)a.cols, a.dweight);
         err = hipGetLastError();
     }
@@ -229,7 +352,7 @@ hipError_t launch_backward(const RmsNormBackwardArgs &a, hipStream_t stream)
 
 int64_t rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols)
 {
-    return (int64_t)parts_of(rows) * cols * (int64_t)sizeof(float);
+    return (int64_t)parts_of(rows, cols) * cols * (int64_t)sizeof(float);
 }
 
 // Makes the runtime load this file's code object
