@@ -39,6 +39,9 @@ _lib = None
 _NATIVE = ("quest_hadamard_quantize", "quest_hadamard_quantize_pair", "quest_hadamard_quantize_fp4",
            "quest_hadamard_quantize_fp4_pair", "quest_lowbit_gemm", "quest_lowbit_gemm_fp4", "quest_trust_backward",
            "quest_trust_backward_pair", "quest_grad_gemm", "quest_grad_gemm_fp4", "quest_weight_only_gemm")
+# those of quest_python.MxCalls
+_MX_NATIVE = ("quest_hadamard_quantize_mx", "quest_dequantize_mx", "quest_lowbit_gemm_mx", "quest_grad_gemm_mx",
+              "quest_rms_norm_mx", "quest_rms_norm_backward")
 
 
 class QuestError(RuntimeError):
@@ -113,7 +116,7 @@ def load():
         lib.quest_container_bits.restype = _i32
         lib.quest_status_string.argtypes = [ctypes.c_int]
         lib.quest_status_string.restype = ctypes.c_char_p
-        lib.calls = _native_calls(lib)
+        lib.calls, lib.mx_calls = _native_calls(lib)
         _lib = lib
     return _lib
 
@@ -124,7 +127,7 @@ def torch_build() -> str:
 
 
 class _NoCalls:
-    """In place of quest_python.Calls: every call takes the ctypes way."""
+    """In place of the native module's objects: every call takes the ctypes way."""
 
     def __getattr__(self, name):
         return lambda *args: None
@@ -135,13 +138,14 @@ def _native_calls(lib):
         from . import quest_python
         built_for = getattr(quest_python, "TORCH_BUILD", "an unknown torch")
         if built_for == torch_build():
-            return quest_python.Calls(*(ctypes.cast(getattr(lib, name), _p).value for name in _NATIVE))
+            return tuple(kind(*(ctypes.cast(getattr(lib, name), _p).value for name in names))
+                         for kind, names in ((quest_python.Calls, _NATIVE), (quest_python.MxCalls, _MX_NATIVE)))
         why = f"it was built for {built_for}, this is {torch_build()}"
     except ImportError as error:
         why = str(error)
     warnings.warn(f"the native module quest_python is not used, calls take 3 us more ({why}); to build it: "
                   "`python -c 'import __graft_entry__ as g; g.build()'`", RuntimeWarning, stacklevel=3)
-    return _NoCalls()
+    return _NoCalls(), _NoCalls()
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -406,7 +410,7 @@ def _current_device() -> int:
 def _check_devices(*tensors: torch.Tensor | None) -> None:
     here = _current_device()
     for t in tensors:
-        if t is not None and (t.device.type != "cuda" or t.device.index != here):
+        if t is not None and t.get_device() != here:   # (-1: in host memory)
             raise ValueError(f"a tensor is on {t.device}, the call runs on cuda:{here}")
 
 
@@ -443,38 +447,51 @@ def quest_hadamard_quantize_mx(x: torch.Tensor, had_block: int, fmt: int, *, cod
                                mask: torch.Tensor | None = None) -> None:
     """x [rows, cols] -> codes [rows, cols/2] (QUEST_MX_E2M1) or [rows, cols] (QUEST_MX_E4M3), a scale byte for each 32 elements
     [rows, cols/32], trust bitmap [rows, cols/8] (uint8, caller-allocated)."""
-    rows, cols, ld = _rows(x, "x")
-    _operand(codes, scales, mask, fmt, rows, cols)
-    _check_devices(x, codes, scales, mask)
-    _check(load().quest_hadamard_quantize_mx(_ptr(x), _dtype_code(x), rows, cols, ld, had_block, fmt, _ptr(codes), _ptr(scales),
-                                             _ptr(mask), _stream()), "quest_hadamard_quantize_mx")
+    status = (_lib or load()).mx_calls.hadamard_quantize_mx(x, had_block, fmt, codes, scales, mask, _stream, _current_device)
+    if status is None:
+        rows, cols, ld = _rows(x, "x")
+        _operand(codes, scales, mask, fmt, rows, cols)
+        _check_devices(x, codes, scales, mask)
+        status = load().quest_hadamard_quantize_mx(_ptr(x), _dtype_code(x), rows, cols, ld, had_block, fmt, _ptr(codes),
+                                                   _ptr(scales), _ptr(mask), _stream())
+    if status:
+        raise QuestError(status, "quest_hadamard_quantize_mx")
 
 
 def quest_dequantize_mx(codes: torch.Tensor, scales: torch.Tensor, fmt: int, *, out: torch.Tensor) -> None:
     """out [rows, cols] (bf16 or fp32): what the codes and scales of quest_hadamard_quantize_mx stand for."""
-    rows, cols, ld = _rows(out, "out")
-    _operand(codes, scales, None, fmt, rows, cols)
-    _check_devices(codes, scales, out)
-    _check(load().quest_dequantize_mx(_ptr(codes), _ptr(scales), fmt, rows, cols, _ptr(out), _dtype_code(out), ld, _stream()),
-           "quest_dequantize_mx")
+    status = (_lib or load()).mx_calls.dequantize_mx(codes, scales, fmt, out, _stream, _current_device)
+    if status is None:
+        rows, cols, ld = _rows(out, "out")
+        _operand(codes, scales, None, fmt, rows, cols)
+        _check_devices(codes, scales, out)
+        status = load().quest_dequantize_mx(_ptr(codes), _ptr(scales), fmt, rows, cols, _ptr(out), _dtype_code(out), ld,
+                                            _stream())
+    if status:
+        raise QuestError(status, "quest_dequantize_mx")
 
 
 def quest_lowbit_gemm_mx(a_codes: torch.Tensor, a_scales: torch.Tensor, a_format: int, b_codes: torch.Tensor,
                          b_scales: torch.Tensor, K: int, *, y: torch.Tensor | None,
                          acc_out: torch.Tensor | None = None) -> None:
     """y[M, N] (bf16) and/or acc_out[M, N] (fp32) = a b^T: activations a in a_format, weights b in QUEST_MX_E2M1."""
-    M, N = a_codes.shape[0], b_codes.shape[0]
-    _operand(a_codes, a_scales, None, a_format, M, K, "a_")
-    _operand(b_codes, b_scales, None, QUEST_MX_E2M1, N, K, "b_")
-    ld_y = N
-    if y is not None:
-        if y.dtype != torch.bfloat16:
-            raise TypeError(f"unsupported tensor dtype {y.dtype}")
-        ld_y = _rows(y, "y", N, M)[2]
-    _packed(acc_out, "acc_out", torch.float32, (M, N))
-    _check_devices(a_codes, a_scales, b_codes, b_scales, y, acc_out)
-    _check(load().quest_lowbit_gemm_mx(_ptr(a_codes), _ptr(a_scales), a_format, M, _ptr(b_codes), _ptr(b_scales), N, K, _ptr(y),
-                                       ld_y, _ptr(acc_out), _stream()), "quest_lowbit_gemm_mx")
+    status = (_lib or load()).mx_calls.lowbit_gemm_mx(a_codes, a_scales, a_format, b_codes, b_scales, K, y, acc_out, _stream,
+                                                      _current_device)
+    if status is None:
+        M, N = a_codes.shape[0], b_codes.shape[0]
+        _operand(a_codes, a_scales, None, a_format, M, K, "a_")
+        _operand(b_codes, b_scales, None, QUEST_MX_E2M1, N, K, "b_")
+        ld_y = N
+        if y is not None:
+            if y.dtype != torch.bfloat16:
+                raise TypeError(f"unsupported tensor dtype {y.dtype}")
+            ld_y = _rows(y, "y", N, M)[2]
+        _packed(acc_out, "acc_out", torch.float32, (M, N))
+        _check_devices(a_codes, a_scales, b_codes, b_scales, y, acc_out)
+        status = load().quest_lowbit_gemm_mx(_ptr(a_codes), _ptr(a_scales), a_format, M, _ptr(b_codes), _ptr(b_scales), N, K,
+                                             _ptr(y), ld_y, _ptr(acc_out), _stream())
+    if status:
+        raise QuestError(status, "quest_lowbit_gemm_mx")
 
 
 def quest_grad_gemm_mx_workspace_bytes(which: int, M: int, N: int, K: int) -> int:
@@ -484,12 +501,17 @@ def quest_grad_gemm_mx_workspace_bytes(which: int, M: int, N: int, K: int) -> in
 def quest_grad_gemm_mx(which: int, dy: torch.Tensor, q_codes: torch.Tensor, q_scales: torch.Tensor, q_format: int, M: int, N: int,
                        K: int, *, out: torch.Tensor, workspace: torch.Tensor | None = None) -> None:
     """quest_grad_gemm for a microscaled operand: weights [N, K] (which = 0) or activations [M, K] (which = 1)."""
-    _packed(dy, "dy", torch.bfloat16, (M, N))
-    _operand(q_codes, q_scales, None, q_format, M if which == 1 else N, K, "q_")
-    _packed(out, "out", torch.bfloat16, (N if which == 1 else M, K))
-    _check_devices(dy, q_codes, q_scales, out, workspace)
-    _check(load().quest_grad_gemm_mx(which, _ptr(dy), _ptr(q_codes), _ptr(q_scales), q_format, M, N, K, _ptr(out),
-                                     _ptr(workspace), _bytes(workspace), _stream()), "quest_grad_gemm_mx")
+    status = (_lib or load()).mx_calls.grad_gemm_mx(which, dy, q_codes, q_scales, q_format, M, N, K, out, workspace, _stream,
+                                                    _current_device)
+    if status is None:
+        _packed(dy, "dy", torch.bfloat16, (M, N))
+        _operand(q_codes, q_scales, None, q_format, M if which == 1 else N, K, "q_")
+        _packed(out, "out", torch.bfloat16, (N if which == 1 else M, K))
+        _check_devices(dy, q_codes, q_scales, out, workspace)
+        status = load().quest_grad_gemm_mx(which, _ptr(dy), _ptr(q_codes), _ptr(q_scales), q_format, M, N, K, _ptr(out),
+                                           _ptr(workspace), _bytes(workspace), _stream())
+    if status:
+        raise QuestError(status, "quest_grad_gemm_mx")
 
 
 def quest_rms_norm_mx(x: torch.Tensor, weight: torch.Tensor, eps: float, had_block: int = 1, fmt: int = QUEST_MX_E4M3, *,
@@ -497,19 +519,24 @@ def quest_rms_norm_mx(x: torch.Tensor, weight: torch.Tensor, eps: float, had_blo
                       residual: torch.Tensor | None = None, h_out: torch.Tensor | None = None, y_out: torch.Tensor | None = None,
                       rstd: torch.Tensor | None = None) -> None:
     """h_out = x + residual; y_out = h * rstd * weight; codes, scales, mask: y as quest_hadamard_quantize_mx quantizes it."""
-    rows, cols, ld_x = _rows(x, "x")
-    ld_residual = _rows(residual, "residual", cols, rows)[2] if residual is not None else 0
-    if residual is not None and residual.dtype != x.dtype:
-        raise TypeError(f"residual is {residual.dtype}, x {x.dtype}")
-    _packed(weight, "weight", weight.dtype, (cols,))
-    _operand(codes, scales, mask, fmt, rows, cols)
-    _packed(h_out, "h_out", x.dtype, (rows, cols))
-    _packed(y_out, "y_out", x.dtype, (rows, cols))
-    _packed(rstd, "rstd", torch.float32, (rows,))
-    _check_devices(x, weight, codes, scales, mask, residual, h_out, y_out, rstd)
-    _check(load().quest_rms_norm_mx(_ptr(x), ld_x, _ptr(residual), ld_residual, _dtype_code(x), _ptr(weight), _dtype_code(weight),
-                                    rows, cols, eps, _ptr(h_out), _ptr(y_out), had_block, fmt, _ptr(codes), _ptr(scales),
-                                    _ptr(mask), _ptr(rstd), _stream()), "quest_rms_norm_mx")
+    status = (_lib or load()).mx_calls.rms_norm_mx(x, weight, eps, had_block, fmt, codes, scales, mask, residual, h_out,
+                                                   y_out, rstd, _stream, _current_device)
+    if status is None:
+        rows, cols, ld_x = _rows(x, "x")
+        ld_residual = _rows(residual, "residual", cols, rows)[2] if residual is not None else 0
+        if residual is not None and residual.dtype != x.dtype:
+            raise TypeError(f"residual is {residual.dtype}, x {x.dtype}")
+        _packed(weight, "weight", weight.dtype, (cols,))
+        _operand(codes, scales, mask, fmt, rows, cols)
+        _packed(h_out, "h_out", x.dtype, (rows, cols))
+        _packed(y_out, "y_out", x.dtype, (rows, cols))
+        _packed(rstd, "rstd", torch.float32, (rows,))
+        _check_devices(x, weight, codes, scales, mask, residual, h_out, y_out, rstd)
+        status = load().quest_rms_norm_mx(_ptr(x), ld_x, _ptr(residual), ld_residual, _dtype_code(x), _ptr(weight),
+                                          _dtype_code(weight), rows, cols, eps, _ptr(h_out), _ptr(y_out), had_block, fmt,
+                                          _ptr(codes), _ptr(scales), _ptr(mask), _ptr(rstd), _stream())
+    if status:
+        raise QuestError(status, "quest_rms_norm_mx")
 
 
 def quest_rms_norm_backward_workspace_bytes(rows: int, cols: int) -> int:
@@ -520,13 +547,18 @@ def quest_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Ten
                             dweight: torch.Tensor | None, dh: torch.Tensor | None = None,
                             workspace: torch.Tensor | None = None) -> None:
     """dx and dweight of quest_rms_norm_mx's y from dy, with dh added to dx (contiguous matrices of one dtype)."""
-    rows, cols, _ = _rows(h, "h")
-    for name, t in (("h", h), ("dy", dy), ("dh", dh), ("dx", dx)):
-        _packed(t, name, h.dtype, (rows, cols))
-    _packed(weight, "weight", weight.dtype, (cols,))
-    _packed(rstd, "rstd", torch.float32, (rows,))
-    _packed(dweight, "dweight", torch.float32, (cols,))
-    _check_devices(dy, h, weight, rstd, dh, dx, dweight, workspace)
-    _check(load().quest_rms_norm_backward(_ptr(dy), _ptr(h), _dtype_code(h), _ptr(weight), _dtype_code(weight), _ptr(rstd),
-                                          _ptr(dh), rows, cols, _ptr(dx), _ptr(dweight), _ptr(workspace), _bytes(workspace),
-                                          _stream()), "quest_rms_norm_backward")
+    status = (_lib or load()).mx_calls.rms_norm_backward(dy, h, weight, rstd, dh, dx, dweight, workspace, _stream,
+                                                         _current_device)
+    if status is None:
+        rows, cols, _ = _rows(h, "h")
+        for name, t in (("h", h), ("dy", dy), ("dh", dh), ("dx", dx)):
+            _packed(t, name, h.dtype, (rows, cols))
+        _packed(weight, "weight", weight.dtype, (cols,))
+        _packed(rstd, "rstd", torch.float32, (rows,))
+        _packed(dweight, "dweight", torch.float32, (cols,))
+        _check_devices(dy, h, weight, rstd, dh, dx, dweight, workspace)
+        status = load().quest_rms_norm_backward(_ptr(dy), _ptr(h), _dtype_code(h), _ptr(weight), _dtype_code(weight),
+                                                _ptr(rstd), _ptr(dh), rows, cols, _ptr(dx), _ptr(dweight), _ptr(workspace),
+                                                _bytes(workspace), _stream())
+    if status:
+        raise QuestError(status, "quest_rms_norm_backward")

@@ -10,6 +10,7 @@
 
 #include <string.h>
 
+#include <initializer_list>
 #include <limits>
 
 #include <ATen/PythonTorchFunctionTLS.h>
@@ -352,21 +353,247 @@ PyObject *weight_only_gemm(PyObject *self, PyObject *const *args, Py_ssize_t cou
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the calls on microscaled operands and of the norm.  binding.py checks shapes, types, strides and places of all tensors of
+// these; here a call is plain if it passes the same checks.
+
+struct MxEntries {
+    decltype(&quest_hadamard_quantize_mx) quantize;
+    decltype(&quest_dequantize_mx) dequantize;
+    decltype(&quest_lowbit_gemm_mx) gemm;
+    decltype(&quest_grad_gemm_mx) grad_gemm;
+    decltype(&quest_rms_norm_mx) rms_norm;
+    decltype(&quest_rms_norm_backward) rms_norm_backward;
+};
+constexpr Py_ssize_t kMxEntries = sizeof(MxEntries) / sizeof(void *);
+
+struct MxCalls {
+    PyObject_HEAD
+    MxEntries entry;
+};
+
+// Reader with those checks; `device` of the methods' arguments: a callable that returns the current device's number
+class MxReader : public Reader {
+public:
+    MxReader(PyObject *const *args, Py_ssize_t count, Py_ssize_t expected) : Reader(args, count, expected) {}
+
+    quest_mx_format format()
+    {
+        const int32_t f = i32();
+        require(f == QUEST_MX_E2M1 || f == QUEST_MX_E4M3);
+        return (quest_mx_format)f;
+    }
+    // a matrix whose rows are contiguous; its row stride
+    int64_t rows_of(const at::Tensor *t, int64_t rows, int64_t cols)
+    {
+        require(plain && t && t->dim() == 2 && t->size(0) == rows && t->size(1) == cols && (cols == 1 || t->stride(1) == 1));
+        return !plain ? 0 : rows > 1 ? t->stride(0) : cols;
+    }
+    void packed(const at::Tensor *t, at::ScalarType type, int64_t rows, int64_t cols)
+    {
+        require(plain && (!t || (t->dim() == 2 && t->scalar_type() == type && t->size(0) == rows && t->size(1) == cols && t->is_contiguous())));
+    }
+    void packed(const at::Tensor *t, at::ScalarType type, int64_t count)
+    {
+        require(plain && (!t || (t->dim() == 1 && t->scalar_type() == type && t->size(0) == count && t->is_contiguous())));
+    }
+    void operand(const at::Tensor *codes, const at::Tensor *scales, const at::Tensor *mask, quest_mx_format format, int64_t rows,
+                 int64_t cols)
+    {
+        packed(codes, at::kByte, rows, format == QUEST_MX_E4M3 ? cols : cols / 2);
+        packed(scales, at::kByte, rows, cols / QUEST_MX_GROUP);
+        packed(mask, at::kByte, rows, cols / 8);
+    }
+    // Whether all tensors are on the device whose number `ask_device` returns (tensors in host memory have the number -1)
+    void on_device(PyObject *ask_device, std::initializer_list<const at::Tensor *> tensors)
+    {
+        if (!plain)
+            return;
+        PyObject *number = PyObject_CallNoArgs(ask_device);
+        const long device = number ? PyLong_AsLong(number) : -1;
+        Py_XDECREF(number);
+        if (PyErr_Occurred()) {
+            PyErr_Clear();   // binding.py asks again, and raises
+            require(false);
+        }
+        for (const at::Tensor *t : tensors)
+            require(!t || t->get_device() == device);
+    }
+};
+
+#define QUEST_MX_ENTRY()                                               \
+    const MxEntries &entry = reinterpret_cast<MxCalls *>(self)->entry; \
+    HANDLE_TH_ERRORS
+
+// (x, had_block, format, codes, scales, mask, stream, device)
+PyObject *mx_quantize(PyObject *self, PyObject *const *args, Py_ssize_t count)
+{
+    QUEST_MX_ENTRY()
+    MxReader r(args, count, 8);
+    const at::Tensor *x = r.matrix();
+    const int32_t block = r.i32();
+    const quest_mx_format format = r.format();
+    const at::Tensor *codes = r.tensor(), *scales = r.tensor(), *mask = r.tensor_or_none();
+    PyObject *ask_stream = r.object(), *ask_device = r.object();
+    const quest_dtype dtype = r.dtype(x);
+    const int64_t rows = r.size(x, 0), cols = r.size(x, 1), ld = r.rows_of(x, rows, cols);
+    r.operand(codes, scales, mask, format, rows, cols);
+    r.on_device(ask_device, {x, codes, scales, mask});
+    QUEST_PLAIN_OR_NONE(r)
+    void *px = pointer(x);
+    uint8_t *pc = pointer(codes), *ps = pointer(scales), *pm = pointer(mask);
+    return enqueue(ask_stream, [&](void *stream) { return entry.quantize(px, dtype, rows, cols, ld, block, format, pc, ps, pm, stream); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (codes, scales, format, out, stream, device)
+PyObject *mx_dequantize(PyObject *self, PyObject *const *args, Py_ssize_t count)
+{
+    QUEST_MX_ENTRY()
+    MxReader r(args, count, 6);
+    const at::Tensor *codes = r.tensor(), *scales = r.tensor();
+    const quest_mx_format format = r.format();
+    const at::Tensor *out = r.matrix();
+    PyObject *ask_stream = r.object(), *ask_device = r.object();
+    const quest_dtype dtype = r.dtype(out);
+    const int64_t rows = r.size(out, 0), cols = r.size(out, 1), ld = r.rows_of(out, rows, cols);
+    r.operand(codes, scales, nullptr, format, rows, cols);
+    r.on_device(ask_device, {codes, scales, out});
+    QUEST_PLAIN_OR_NONE(r)
+    uint8_t *pc = pointer(codes), *ps = pointer(scales);
+    void *po = pointer(out);
+    return enqueue(ask_stream, [&](void *stream) { return entry.dequantize(pc, ps, format, rows, cols, po, dtype, ld, stream); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (a_codes, a_scales, a_format, b_codes, b_scales, K, y, acc_out, stream, device)
+PyObject *mx_gemm(PyObject *self, PyObject *const *args, Py_ssize_t count)
+{
+    QUEST_MX_ENTRY()
+    MxReader r(args, count, 10);
+    const at::Tensor *a = r.tensor(), *a_scales = r.tensor();
+    const quest_mx_format format = r.format();
+    const at::Tensor *b = r.tensor(), *b_scales = r.tensor();
+    const int64_t K = r.i64();
+    const at::Tensor *y = r.tensor_or_none(), *acc = r.tensor_or_none();
+    PyObject *ask_stream = r.object(), *ask_device = r.object();
+    const int64_t M = r.size(a, 0), N = r.size(b, 0);
+    r.operand(a, a_scales, nullptr, format, M, K);
+    r.operand(b, b_scales, nullptr, QUEST_MX_E2M1, N, K);
+    r.require(!y || y->scalar_type() == at::kBFloat16);
+    const int64_t ld_y = y ? r.rows_of(y, M, N) : N;
+    r.packed(acc, at::kFloat, M, N);
+    r.on_device(ask_device, {a, a_scales, b, b_scales, y, acc});
+    QUEST_PLAIN_OR_NONE(r)
+    uint8_t *pa = pointer(a), *sa = pointer(a_scales), *pb = pointer(b), *sb = pointer(b_scales);
+    void *py = pointer(y);
+    float *pacc = pointer<float>(acc);
+    return enqueue(ask_stream, [&](void *stream) { return entry.gemm(pa, sa, format, M, pb, sb, N, K, py, ld_y, pacc, stream); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (which, dy, q_codes, q_scales, format, M, N, K, out, workspace, stream, device)
+PyObject *mx_grad_gemm(PyObject *self, PyObject *const *args, Py_ssize_t count)
+{
+    QUEST_MX_ENTRY()
+    MxReader r(args, count, 12);
+    const int32_t which = r.i32();
+    const at::Tensor *dy = r.tensor(), *codes = r.tensor(), *scales = r.tensor();
+    const quest_mx_format format = r.format();
+    const int64_t M = r.i64(), N = r.i64(), K = r.i64();
+    const at::Tensor *out = r.tensor(), *workspace = r.tensor_or_none();
+    PyObject *ask_stream = r.object(), *ask_device = r.object();
+    r.packed(dy, at::kBFloat16, M, N);
+    r.operand(codes, scales, nullptr, format, which == 1 ? M : N, K);
+    r.packed(out, at::kBFloat16, which == 1 ? N : M, K);
+    r.on_device(ask_device, {dy, codes, scales, out, workspace});
+    QUEST_PLAIN_OR_NONE(r)
+    void *pdy = pointer(dy), *po = pointer(out), *pws = pointer(workspace);
+    uint8_t *pc = pointer(codes), *ps = pointer(scales);
+    const int64_t scratch = bytes(workspace);
+    return enqueue(ask_stream, [&](void *stream) { return entry.grad_gemm(which, pdy, pc, ps, format, M, N, K, po, pws, scratch, stream); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, weight, eps, had_block, format, codes, scales, mask, residual, h_out, y_out, rstd, stream, device)
+PyObject *mx_rms_norm(PyObject *self, PyObject *const *args, Py_ssize_t count)
+{
+    QUEST_MX_ENTRY()
+    MxReader r(args, count, 14);
+    const at::Tensor *x = r.matrix(), *weight = r.tensor();
+    const float eps = r.f32();
+    const int32_t block = r.i32();
+    const quest_mx_format format = r.format();
+    const at::Tensor *codes = r.tensor_or_none(), *scales = r.tensor_or_none(), *mask = r.tensor_or_none();
+    const at::Tensor *residual = r.tensor_or_none(), *h = r.tensor_or_none(), *y = r.tensor_or_none(), *rstd = r.tensor_or_none();
+    PyObject *ask_stream = r.object(), *ask_device = r.object();
+    const quest_dtype dtype = r.dtype(x), weight_dtype = r.dtype(weight);
+    const int64_t rows = r.size(x, 0), cols = r.size(x, 1), ld_x = r.rows_of(x, rows, cols);
+    r.require(r.plain && (!residual || residual->scalar_type() == x->scalar_type()));
+    const int64_t ld_residual = residual ? r.rows_of(residual, rows, cols) : 0;
+    r.operand(codes, scales, mask, format, rows, cols);
+    if (r.plain) {
+        r.packed(weight, weight->scalar_type(), cols);
+        r.packed(h, x->scalar_type(), rows, cols);
+        r.packed(y, x->scalar_type(), rows, cols);
+        r.packed(rstd, at::kFloat, rows);
+    }
+    r.on_device(ask_device, {x, weight, codes, scales, mask, residual, h, y, rstd});
+    QUEST_PLAIN_OR_NONE(r)
+    void *px = pointer(x), *pr = pointer(residual), *pw = pointer(weight), *ph = pointer(h), *py = pointer(y);
+    uint8_t *pc = pointer(codes), *ps = pointer(scales), *pm = pointer(mask);
+    float *pt = pointer<float>(rstd);
+    return enqueue(ask_stream, [&](void *stream) {
+        return entry.rms_norm(px, ld_x, pr, ld_residual, dtype, pw, weight_dtype, rows, cols, eps, ph, py, block, format, pc, ps, pm, pt,
+                              stream);
+    });
+    END_HANDLE_TH_ERRORS
+}
+
+// (dy, h, weight, rstd, dh, dx, dweight, workspace, stream, device)
+PyObject *mx_rms_norm_backward(PyObject *self, PyObject *const *args, Py_ssize_t count)
+{
+    QUEST_MX_ENTRY()
+    MxReader r(args, count, 10);
+    const at::Tensor *dy = r.matrix(), *h = r.matrix(), *weight = r.tensor(), *rstd = r.tensor(), *dh = r.tensor_or_none();
+    const at::Tensor *dx = r.tensor(), *dweight = r.tensor_or_none(), *workspace = r.tensor_or_none();
+    PyObject *ask_stream = r.object(), *ask_device = r.object();
+    const quest_dtype dtype = r.dtype(h), weight_dtype = r.dtype(weight);
+    const int64_t rows = r.size(h, 0), cols = r.size(h, 1);
+    if (r.plain) {
+        for (const at::Tensor *t : {h, dy, dh, dx})
+            r.packed(t, h->scalar_type(), rows, cols);
+        r.packed(weight, weight->scalar_type(), cols);
+        r.packed(rstd, at::kFloat, rows);
+        r.packed(dweight, at::kFloat, cols);
+    }
+    r.on_device(ask_device, {dy, h, weight, rstd, dh, dx, dweight, workspace});
+    QUEST_PLAIN_OR_NONE(r)
+    void *pdy = pointer(dy), *ph = pointer(h), *pw = pointer(weight), *pdh = pointer(dh), *pdx = pointer(dx), *pws = pointer(workspace);
+    float *pt = pointer<float>(rstd), *pdw = pointer<float>(dweight);
+    const int64_t scratch = bytes(workspace);
+    return enqueue(ask_stream, [&](void *stream) {
+        return entry.rms_norm_backward(pdy, ph, dtype, pw, weight_dtype, pt, pdh, rows, cols, pdx, pdw, pws, scratch, stream);
+    });
+    END_HANDLE_TH_ERRORS
+}
+
 #undef QUEST_ENTRY
+#undef QUEST_MX_ENTRY
 #undef QUEST_PLAIN_OR_NONE
 
-// Calls(addresses of the entry points in the order of Entries)
+// Object(addresses of the entry points in the order of Table)
+template <typename Object, typename Table, Py_ssize_t COUNT>
 PyObject *new_calls(PyTypeObject *type, PyObject *args, PyObject *)
 {
-    if (PyTuple_GET_SIZE(args) != kEntries) {
+    if (PyTuple_GET_SIZE(args) != COUNT) {
         PyErr_SetString(PyExc_TypeError, "one address for each entry point");
         return nullptr;
     }
-    auto *self = reinterpret_cast<Calls *>(type->tp_alloc(type, 0));
+    auto *self = reinterpret_cast<Object *>(type->tp_alloc(type, 0));
     if (!self)
         return nullptr;
-    void *address[kEntries];
-    for (Py_ssize_t i = 0; i < kEntries; ++i) {
+    void *address[COUNT];
+    for (Py_ssize_t i = 0; i < COUNT; ++i) {
         address[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(args, i));
         if (!address[i]) {
             if (!PyErr_Occurred())
@@ -375,7 +602,7 @@ PyObject *new_calls(PyTypeObject *type, PyObject *args, PyObject *)
             return nullptr;
         }
     }
-    memcpy(&self->entry, address, sizeof(Entries));
+    memcpy(&self->entry, address, sizeof(Table));
     return reinterpret_cast<PyObject *>(self);
 }
 
@@ -392,19 +619,29 @@ PyMethodDef methods[] = {QUEST_METHOD("hadamard_quantize", hadamard_quantize),
                          QUEST_METHOD("grad_gemm_fp4", grad_gemm<true>),
                          QUEST_METHOD("weight_only_gemm", weight_only_gemm),
                          {nullptr, nullptr, 0, nullptr}};
+PyMethodDef mx_methods[] = {QUEST_METHOD("hadamard_quantize_mx", mx_quantize),
+                            QUEST_METHOD("dequantize_mx", mx_dequantize),
+                            QUEST_METHOD("lowbit_gemm_mx", mx_gemm),
+                            QUEST_METHOD("grad_gemm_mx", mx_grad_gemm),
+                            QUEST_METHOD("rms_norm_mx", mx_rms_norm),
+                            QUEST_METHOD("rms_norm_backward", mx_rms_norm_backward),
+                            {nullptr, nullptr, 0, nullptr}};
 #undef QUEST_METHOD
 
 PyTypeObject calls_type = {PyVarObject_HEAD_INIT(nullptr, 0) "quest_python.Calls", sizeof(Calls)};
+PyTypeObject mx_calls_type = {PyVarObject_HEAD_INIT(nullptr, 0) "quest_python.MxCalls", sizeof(MxCalls)};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "quest_python", nullptr, -1, nullptr};
 
 }  // namespace
 
 PyMODINIT_FUNC PyInit_quest_python(void)
 {
-    calls_type.tp_flags = Py_TPFLAGS_DEFAULT;
+    calls_type.tp_flags = mx_calls_type.tp_flags = Py_TPFLAGS_DEFAULT;
     calls_type.tp_methods = methods;
-    calls_type.tp_new = new_calls;
-    if (PyType_Ready(&calls_type) < 0)
+    calls_type.tp_new = new_calls<Calls, Entries, kEntries>;
+    mx_calls_type.tp_methods = mx_methods;
+    mx_calls_type.tp_new = new_calls<MxCalls, MxEntries, kMxEntries>;
+    if (PyType_Ready(&calls_type) < 0 || PyType_Ready(&mx_calls_type) < 0)
         return nullptr;
     PyObject *m = PyModule_Create(&module);
     if (!m)
@@ -413,11 +650,17 @@ PyMODINIT_FUNC PyInit_quest_python(void)
         Py_DECREF(m);
         return nullptr;
     }
-    Py_INCREF(&calls_type);
-    if (PyModule_AddObject(m, "Calls", reinterpret_cast<PyObject *>(&calls_type)) < 0) {
-        Py_DECREF(&calls_type);
-        Py_DECREF(m);
-        return nullptr;
+    const struct {
+        const char *name;
+        PyTypeObject *type;
+    } types[] = {{"Calls", &calls_type}, {"MxCalls", &mx_calls_type}};
+    for (const auto &t : types) {
+        Py_INCREF(t.type);
+        if (PyModule_AddObject(m, t.name, reinterpret_cast<PyObject *>(t.type)) < 0) {
+            Py_DECREF(t.type);
+            Py_DECREF(m);
+            return nullptr;
+        }
     }
     return m;
 }

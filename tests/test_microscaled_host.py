@@ -1,6 +1,8 @@
 """Microscaled operands and the norm without a GPU: refusals of the C entry points and of the binding, and pins of the 64-bit
 definitions that the GPU tests compare with."""
 import ctypes
+import inspect
+import types
 
 import numpy as np
 import pytest
@@ -176,6 +178,113 @@ def test_binding_refuses_tensors_elsewhere(monkeypatch):
                  lambda: q.quest_rms_norm_backward(x, x, w, rstd, dx=x, dweight=None)):
         with pytest.raises(ValueError, match="is on cpu"):
             call()
+
+
+# ---- the two ways to an entry point, native code and ctypes (stand-ins record what they are given)
+
+def mx_calls(dtype):
+    """name, positional, keyword arguments: forms and options of every call; tensors in host memory"""
+    x, wide, w = torch.zeros(4, 64, dtype=dtype), torch.zeros(4, 96, dtype=dtype), torch.zeros(64)
+    quantized = dict(codes=u8(4, 32), scales=u8(4, 2))
+    yield "quest_hadamard_quantize_mx", (x, 32, 0), quantized
+    yield "quest_hadamard_quantize_mx", (wide[:, :64], 1, 1), dict(codes=u8(4, 64), scales=u8(4, 2), mask=u8(4, 8))
+    yield "quest_hadamard_quantize_mx", (wide[1:2, :64], 1, 0), dict(codes=u8(1, 32), scales=u8(1, 2))
+    yield "quest_hadamard_quantize_mx", (x[:0], 1, 0), dict(codes=u8(0, 32), scales=u8(0, 2))
+    yield "quest_dequantize_mx", (u8(4, 32), u8(4, 2), 0), dict(out=wide[:, :64])
+    a, s, b, t, y = u8(4, 128), u8(4, 4), u8(6, 64), u8(6, 4), torch.zeros(4, 9, dtype=torch.bfloat16)
+    yield "quest_lowbit_gemm_mx", (a, s, 1, b, t, 128), dict(y=y[:, :6])
+    yield "quest_lowbit_gemm_mx", (a[:, :64].contiguous(), s, 0, b, t, 128), dict(y=None, acc_out=torch.zeros(4, 6))
+    dy, scratch = torch.zeros(128, 192, dtype=torch.bfloat16), torch.zeros(33, dtype=torch.int16)
+    yield "quest_grad_gemm_mx", (0, dy, u8(192, 64), u8(192, 4), 0, 128, 192, 128), dict(out=torch.zeros(128, 128, dtype=torch.bfloat16))
+    yield ("quest_grad_gemm_mx", (1, dy, u8(128, 128), u8(128, 4), 1, 128, 192, 128),
+           dict(out=torch.zeros(192, 128, dtype=torch.bfloat16), workspace=scratch))
+    yield "quest_rms_norm_mx", (x, w, 1e-5, 32, 0), quantized
+    yield ("quest_rms_norm_mx", (wide[:, :64], w.bfloat16(), 1e-6, 1, 1),
+           dict(codes=u8(4, 64), scales=u8(4, 2), mask=u8(4, 8), residual=wide[:, 32:], h_out=x, y_out=x.clone(), rstd=torch.zeros(4)))
+    yield "quest_rms_norm_mx", (x, w, 1e-5), dict(y_out=x.clone())
+    yield "quest_rms_norm_backward", (x, x, w, torch.zeros(4)), dict(dx=x.clone(), dweight=None)
+    yield ("quest_rms_norm_backward", (x, x, w.bfloat16(), torch.zeros(4)),
+           dict(dx=x.clone(), dweight=w.clone(), dh=x.clone(), workspace=scratch))
+
+
+@pytest.fixture
+def record(monkeypatch):
+    seen, keep = [], {}
+    real = q.load()
+
+    def entry(name):
+        def called(*args):
+            seen.append((name, args))
+            return 0
+        return ctypes.CFUNCTYPE(ctypes.c_int, *getattr(real, name).argtypes)(called)
+    keep.update({name: entry(name) for name in q._MX_NATIVE})
+    from paper_2502_05003_amd import quest_python
+    native = quest_python.MxCalls(*(ctypes.cast(f, ctypes.c_void_p).value for f in keep.values()))
+    refuses = types.SimpleNamespace(**{name: lambda *args: None for name in dir(native) if not name.startswith("_")})
+    library = types.SimpleNamespace(mx_calls=native, quest_status_string=real.quest_status_string, **keep)
+    monkeypatch.setattr(q, "_lib", library)
+    monkeypatch.setattr(q, "_stream", lambda: 0x7fff_1234_5678)
+    monkeypatch.setattr(q, "_current_device", lambda: -1)          # what tensors in host memory say
+    return types.SimpleNamespace(seen=seen, native=native, refuses=refuses, library=library, keep=keep)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_both_ways_pass_the_same_arguments(record, dtype):
+    named = set()
+    for name, args, kwargs in mx_calls(dtype):
+        record.library.mx_calls = record.native
+        assert getattr(q, name)(*args, **kwargs) is None
+        record.library.mx_calls = record.refuses
+        getattr(q, name)(*args, **kwargs)
+        native, general = record.seen[-2:]
+        assert native[0] == general[0] == name and native[1] == general[1], name
+        named.add(name)
+    assert named == set(q._MX_NATIVE) and len(record.seen) % 2 == 0
+
+
+def test_plain_calls_are_native_ones(record):
+    for name in q._MX_NATIVE:
+        setattr(record.library, name, None)
+    for name, args, kwargs in mx_calls(torch.bfloat16):
+        getattr(q, name)(*args, **kwargs)
+    assert len(record.seen) == len(list(mx_calls(torch.bfloat16)))
+
+
+def test_what_is_refused_reaches_no_entry_point(record, monkeypatch):
+    """The native way gives the calls of the tests above to the general one, which raises."""
+    test_binding_refuses_other_shapes_types_and_places()
+    monkeypatch.setattr(q, "_current_device", lambda: 0)
+    for name, args, kwargs in mx_calls(torch.bfloat16):
+        with pytest.raises(ValueError, match="is on cpu"):
+            getattr(q, name)(*args, **kwargs)
+
+    def fails():
+        raise RuntimeError("no device")
+    monkeypatch.setattr(q, "_current_device", fails)
+    for name, args, kwargs in mx_calls(torch.bfloat16):
+        with pytest.raises(RuntimeError, match="no device"):
+            getattr(q, name)(*args, **kwargs)
+    assert not record.seen
+
+
+SIGNATURES = {
+    "quest_hadamard_quantize_mx": ("x had_block fmt", "codes scales mask=None"),
+    "quest_dequantize_mx": ("codes scales fmt", "out"),
+    "quest_lowbit_gemm_mx": ("a_codes a_scales a_format b_codes b_scales K", "y acc_out=None"),
+    "quest_grad_gemm_mx": ("which dy q_codes q_scales q_format M N K", "out workspace=None"),
+    "quest_rms_norm_mx": ("x weight eps had_block=1 fmt=1",
+                          "codes=None scales=None mask=None residual=None h_out=None y_out=None rstd=None"),
+    "quest_rms_norm_backward": ("dy h weight rstd", "dx dweight dh=None workspace=None"),
+}
+
+
+def test_signatures():
+    assert set(q._MX_NATIVE) == set(SIGNATURES)
+    for name, expected in SIGNATURES.items():
+        kinds = {inspect.Parameter.POSITIONAL_OR_KEYWORD: [], inspect.Parameter.KEYWORD_ONLY: []}
+        for p in inspect.signature(getattr(q, name)).parameters.values():
+            kinds[p.kind].append(p.name if p.default is p.empty else f"{p.name}={p.default}")
+        assert tuple(" ".join(names) for names in kinds.values()) == expected, name
 
 
 # ---- the definitions
