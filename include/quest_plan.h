@@ -17,7 +17,7 @@ typedef enum {
     QUEST_PLAN_GENERAL = 0,    /* hq_generic_kernel, lowbit_gemm_kernel */
     QUEST_PLAN_INSTANCE = 1,   /* quantizer: hq_mfma_kernel */
     QUEST_PLAN_ROWS = 2,       /* quantizer: hq_rows_kernel */
-    QUEST_PLAN_FEW = 3,        /* forward product: skinny_gemm_kernel */
+    QUEST_PLAN_FEW = 3,        /* forward product: skinny_gemm_kernel, mx_few_kernel */
     QUEST_PLAN_TILES = 4,      /* products: tile kernels (whole tiles) */
     QUEST_PLAN_SPLIT = 5,      /* 16-bit products: tiles split over the compute units, then the fix-up kernel */
     QUEST_PLAN_MID = 6         /* 16-bit products: grad_gemm_mid_kernel */
@@ -49,6 +49,9 @@ typedef struct {
     int32_t block_rows, block_cols, in_flight, waves;
 } quest_plan_few;
 quest_plan_few quest_plan_forward_few(int32_t bits, int64_t M, int64_t N, int64_t K);
+
+/* quest_lowbit_gemm_mx, either format: FEW (mx_few_kernel) or TILES (mx_tile_kernel) and its block */
+quest_plan quest_plan_mx_gemm(int64_t M, int64_t N, int64_t K);
 
 /* quest_hadamard_quantize (mode 0), _absmax (1) and _fp4 (2); rows: of both operands; f32: fp32 rows */
 quest_plan quest_plan_quantize(int32_t mode, int32_t f32, int64_t rows, int64_t cols, int32_t had_block, int32_t bits);

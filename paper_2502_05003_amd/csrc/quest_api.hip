@@ -850,6 +850,10 @@ quest_status quest_init(void)
         if (err == hipSuccess)
             err = quest::prepare_mx_gemm_kernels();
         if (err == hipSuccess)
+            err = quest::prepare_mx_tiles_e2m1_kernels();
+        if (err == hipSuccess)
+            err = quest::prepare_mx_tiles_e4m3_kernels();
+        if (err == hipSuccess)
             err = quest::prepare_rms_norm_kernels();
         void *ptr = nullptr;
         if (err == hipSuccess)

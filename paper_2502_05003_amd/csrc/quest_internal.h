@@ -129,6 +129,10 @@ struct MxGemmArgs {
     float *acc_out;   // may be null
 };
 hipError_t launch_mx_gemm(const MxGemmArgs &a, hipStream_t stream);
+quest_plan plan_mx_gemm(int64_t M, int64_t N, int64_t K);
+// Its tile kernels, by the activations' format; `block`: 256 or 128
+hipError_t launch_mx_tiles_e2m1(const MxGemmArgs &a, int block, hipStream_t stream);
+hipError_t launch_mx_tiles_e4m3(const MxGemmArgs &a, int block, hipStream_t stream);
 
 struct RmsNormArgs {
     const void *x;
@@ -250,6 +254,8 @@ hipError_t prepare_grad_gemm_kernels();
 hipError_t prepare_grad_gemm_mid_kernels();
 hipError_t prepare_mx_quantize_kernels();
 hipError_t prepare_mx_gemm_kernels();
+hipError_t prepare_mx_tiles_e2m1_kernels();
+hipError_t prepare_mx_tiles_e4m3_kernels();
 hipError_t prepare_rms_norm_kernels();
 
 // Runs a set-up step until it has succeeded once on the current device; afterwards the cost is the question

@@ -186,7 +186,8 @@ def product_bound(a, b, fmt):
 
 
 PRODUCTS = [(1, 1, 128), (1, 5632, 2048), (7, 33, 384), (16, 640, 5632), (24, 96, 1024), (65, 130, 256), (130, 257, 128),
-            (333, 512, 1024), (300, 1283, 640), (1030, 520, 512)]
+            (333, 512, 1024), (300, 1283, 640), (1030, 520, 512), (32, 4096, 256), (200, 1024, 384), (256, 2040, 256), (300, 2100, 384),
+            (40, 9000, 512)]
 
 
 @pytest.mark.parametrize("M,N,K", PRODUCTS)
@@ -216,7 +217,11 @@ def sampled(count, rng):
     return np.array(sorted(i for i in at if 0 <= i < count))
 
 
-@pytest.mark.parametrize("M,N,K", [(2100, 2200, 512), (2100, 2200, 640), (2303, 2056, 1152), (4097, 1288, 2048), (1800, 5128, 768)])
+LARGE_PRODUCTS = [(2100, 2200, 512), (2100, 2200, 640), (2303, 2056, 1152), (4097, 1288, 2048), (1800, 5128, 768), (2600, 4104, 512),
+                  (2600, 4104, 640), (6000, 4104, 1152)]
+
+
+@pytest.mark.parametrize("M,N,K", LARGE_PRODUCTS)
 @pytest.mark.parametrize("fmt", [E2M1, E4M3])
 def test_large_product(M, N, K, fmt):
     """Sampled rows and columns by the bound, all outputs by their norm; the same bits whatever else is asked for."""
@@ -235,6 +240,7 @@ def test_large_product(M, N, K, fmt):
     whole = torch.from_numpy(a).to(DEV) @ torch.from_numpy(b).to(DEV).t()
     # what the matrix instruction drops with E4M3 is below 2^-13 of a group's largest product: a few of 32 are that large
     assert float((acc.double() - whole).norm()) <= (2.0 ** -20 if fmt == E2M1 else 2.0 ** -12) * float(whole.norm())
+    del whole
     odd = torch.full((M, N + 3), -7.0, dtype=BF16, device=DEV)
     q.quest_lowbit_gemm_mx(dev[0], dev[1], fmt, dev[2], dev[3], K, y=odd[:, :N])
     assert torch.equal(odd[:, :N], y) and bool((odd[:, N:] == -7.0).all())

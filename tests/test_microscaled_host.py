@@ -344,3 +344,27 @@ def test_norm_gradient_against_differences():
         step[1, j] = 1e-6
         assert dx[1, j] == pytest.approx((loss(h + step, w) - loss(h - step, w)) / 2e-6, rel=1e-6, abs=1e-8)
         assert dw[j] == pytest.approx((loss(h, w + step[1]) - loss(h, w - step[1])) / 2e-6, rel=1e-6, abs=1e-8)
+
+
+# ---- which kernel a product gets
+
+def mx_plan(M, N, K):
+    import plan
+    ask = q.load().quest_plan_mx_gemm
+    ask.argtypes, ask.restype = [ctypes.c_int64] * 3, plan._Plan
+    p = ask(M, N, K)
+    return {plan.FEW: "few", plan.TILES: "tiles"}[p.kernel], p.block_rows, p.block_cols
+
+
+def test_products_reach_every_kernel():
+    """The shapes of the GPU tests cover all blocks; short contractions and few rows keep off the tiles."""
+    import test_gpu_microscaled as gpu
+    reached = {mx_plan(*shape) for shape in gpu.PRODUCTS + gpu.LARGE_PRODUCTS}
+    assert reached == {("few", 16, 16), ("few", 16, 32), ("few", 32, 32), ("few", 64, 32), ("few", 64, 64), ("tiles", 128, 128),
+                       ("tiles", 256, 256)}
+    for block in (128, 256):        # with workgroups that go on to another tile, and contractions of two stages, of whole ones and a half
+        of = [s for s in gpu.LARGE_PRODUCTS if mx_plan(*s)[1] == block]
+        assert any(-(-M // block) * -(-N // block) > 256 for M, N, K in of)
+        assert {K % 256 for M, N, K in of} == {0, 128} and 512 in {K for M, N, K in of}
+    assert mx_plan(1, 1 << 22, 65536)[0] == "few" and mx_plan(1 << 22, 1 << 22, 384) == ("few", 64, 64)
+    assert mx_plan(1 << 22, 1 << 22, 512) == ("tiles", 256, 256)
