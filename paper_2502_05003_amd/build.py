@@ -14,7 +14,7 @@ PROBE_LIB = os.path.join(_HERE, "libquest_probe.so")   # measurement aid of benc
 SOURCES = ["quest_api.hip", "hadamard_quantize.hip", "hadamard_quantize_mfma.hip", "hadamard_quantize_rows.hip",
            "lowbit_gemm.hip", "skinny_gemm.hip", "fp4_gemm.hip", "trust_backward.hip", "trust_backward_mfma.hip",
            "trust_backward_rows.hip", "grad_gemm.hip",
-           "grad_gemm_mid.hip", "mx_quantize.hip", "mx_gemm.hip",
+           "grad_gemm_mid.hip", "grad_gemm_mid_mx.hip", "mx_quantize.hip", "mx_gemm.hip",
            "mx_tiles_e2m1.hip", "mx_tiles_e4m3.hip", "rms_norm.hip"]
 # per-source extra flags: kernels whose MFMA results are consumed by vector code keep them in VGPRs
 EXTRA_FLAGS = {"hadamard_quantize_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],

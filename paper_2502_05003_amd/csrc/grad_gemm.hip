@@ -697,7 +697,7 @@ struct GradGemmPlan {
     size_t expanded_bytes, partial_bytes;
 };
 
-// grid: 1 .. 4 bits of the Eq. 1 grid, 0 E2M1; what scratch the plan needs does not depend on it
+// grid: 1 .. 4 bits of the Eq. 1 grid, 0 E2M1, kGridMx + format microscaled; what scratch the plan needs does not depend on it
 GradGemmPlan plan_grad_gemm(int which, int grid, int64_t M, int64_t N, int64_t K, int cus)
 {
     GradGemmPlan p = {};
@@ -877,11 +877,13 @@ hipError_t launch_grad_gemm(const GradGemmArgs &a, hipStream_t stream)
         return hipSuccess;
     const auto *dy = static_cast<const uint16_t *>(a.dy);
     auto *out = static_cast<uint16_t *>(a.out);
-    const GradGemmPlan p = plan_grad_gemm(a.which, a.fp4 ? 0 : a.bits, a.M, a.N, a.K, device_compute_units());
+    const int grid = a.mx_scales ? kGridMx + (int)a.mx_format : a.fp4 ? 0 : a.bits;
+    const GradGemmPlan p = plan_grad_gemm(a.which, grid, a.M, a.N, a.K, device_compute_units());
     if (!p.covered)
         return hipErrorInvalidValue;
-    if (p.mid && a.mx_scales == nullptr) {
-        const GradMidArgs mid = {a.which, a.fp4 ? 0 : a.bits, a.dy, p.ld_left, a.q_codes, a.K * a.cb / 8, a.q_scales,
+    if (p.mid) {
+        const void *scales = a.mx_scales ? static_cast<const void *>(a.mx_scales) : a.q_scales;
+        const GradMidArgs mid = {a.which, grid, a.dy, p.ld_left, a.q_codes, a.K * a.cb / 8, scales,
                                  p.contraction, p.out_rows, p.out_cols, a.out};
         return launch_grad_gemm_mid(mid, stream);
     }

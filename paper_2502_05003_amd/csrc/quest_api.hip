@@ -721,7 +721,7 @@ quest_status quest_lowbit_gemm_mx(const uint8_t *a_codes, const uint8_t *a_scale
 
 int64_t quest_grad_gemm_mx_workspace_bytes(int32_t which, int64_t M, int64_t N, int64_t K)
 {
-    return quest_grad_gemm_fp4_workspace_bytes(which, M, N, K);   // the expanded operand is the same
+    return quest_grad_gemm_workspace_bytes(which, M, N, K);   // the expanded operand is the same
 }
 
 quest_status quest_grad_gemm_mx(int32_t which, const void *dy, const uint8_t *q_codes, const uint8_t *q_scales,
@@ -744,7 +744,7 @@ quest_status quest_grad_gemm_mx(int32_t which, const void *dy, const uint8_t *q_
 
     quest::GradGemmArgs args;
     args.which = which;
-    args.fp4 = true;
+    args.fp4 = false;
     args.dy = dy;
     args.q_codes = q_codes;
     args.q_scales = nullptr;
@@ -845,6 +845,8 @@ quest_status quest_init(void)
             err = quest::prepare_grad_gemm_kernels();
         if (err == hipSuccess)
             err = quest::prepare_grad_gemm_mid_kernels();
+        if (err == hipSuccess)
+            err = quest::prepare_grad_gemm_mid_mx_kernels();
         if (err == hipSuccess)
             err = quest::prepare_mx_quantize_kernels();
         if (err == hipSuccess)

@@ -208,20 +208,23 @@ struct GradGemmArgs {
 };
 
 // The same products for outputs of few tiles (grad_gemm_mid.hip); needs no scratch.
+constexpr int kGridMx = 5;
 struct GradMidArgs {
     int mode;            // as GradGemmArgs::which
-    int grid;            // 1 .. 4: bits of the Eq. 1 grid; 0: E2M1
+    int grid;            // 1 .. 4: bits of the Eq. 1 grid; 0: E2M1; kGridMx + format: microscaled
     const void *left;    // bf16: dy, or x for the weight-only product
     int64_t ld_left;
     const uint8_t *q_codes;
     int64_t q_row_bytes;
-    const float *q_scales;
+    const void *q_scales;   // fp32, or bytes (microscaled)
     int64_t C, R, K;     // contraction length, output rows and columns
     void *out;
 };
 
-// every shape of multiples of 64; E2M1 codes for modes 0 and 1 only
+// every shape of multiples of 64; E2M1 and microscaled codes for modes 0 and 1 only
 hipError_t launch_grad_gemm_mid(const GradMidArgs &a, hipStream_t stream);
+// its kernels for microscaled operands; `shape`: the number of the block that was chosen
+hipError_t launch_grad_gemm_mid_mx(const GradMidArgs &a, int shape, hipStream_t stream);
 // the block of the kernel the call gets (kernel, block_rows, block_cols, count)
 quest_plan grad_gemm_mid_plan(int grid, int64_t C, int64_t R, int64_t K, int cus);
 // what the call is expected to take, us
@@ -252,6 +255,7 @@ hipError_t prepare_fp4_gemm_kernels();
 hipError_t prepare_trust_backward_kernels();
 hipError_t prepare_grad_gemm_kernels();
 hipError_t prepare_grad_gemm_mid_kernels();
+hipError_t prepare_grad_gemm_mid_mx_kernels();
 hipError_t prepare_mx_quantize_kernels();
 hipError_t prepare_mx_gemm_kernels();
 hipError_t prepare_mx_tiles_e2m1_kernels();

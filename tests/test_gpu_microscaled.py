@@ -309,14 +309,20 @@ def test_empty_products():
 # ---- gradients
 
 def grad_scratch(which, M, N, K):
-    return torch.full((q.quest_grad_gemm_mx_workspace_bytes(which, M, N, K),), 0xC3, dtype=torch.uint8, device=DEV)
+    nbytes = q.quest_grad_gemm_mx_workspace_bytes(which, M, N, K)
+    return torch.full((nbytes,), 0xC3, dtype=torch.uint8, device=DEV) if nbytes else None
 
 
-@pytest.mark.parametrize("M,N,K", [(128, 128, 128), (192, 320, 448), (512, 128, 640), (2048, 448, 192), (128, 2048, 256)])
+GRADIENTS = [(64, 64, 64), (64, 192, 128), (128, 128, 128), (192, 320, 448), (512, 128, 640), (2048, 448, 192), (128, 2048, 256),
+             (1024, 768, 512), (704, 1472, 1600), (2624, 1344, 1728)]
+
+
+@pytest.mark.parametrize("M,N,K", GRADIENTS)
 @pytest.mark.parametrize("fmt", [E2M1, E4M3])
 @pytest.mark.parametrize("which", [0, 1])
 def test_gradient_products(M, N, K, fmt, which):
     codes, scales = random_operand(M if which else N, K, fmt, K)
+    scales[1, 0] = 0                       # 2^-127: not a normal number by itself
     v = mx.values(codes, scales, fmt)
     rng = np.random.default_rng(M)
     dy = torch.from_numpy((0.03 * rng.standard_normal((M, N))).astype(np.float32)).to(BF16)
@@ -329,6 +335,18 @@ def test_gradient_products(M, N, K, fmt, which):
     # fp32 accumulation over the contraction, one rounding to bf16
     bound = 2.0 ** -8 * np.abs(ref) + 2 * left.shape[1] * 2.0 ** -24 * (np.abs(left) @ np.abs(v))
     assert np.all(np.abs(to_host_f64(out) - ref) <= bound)
+
+
+@pytest.mark.parametrize("M,N,K", [(128, 192, 128), (4096, 1600, 1280)])
+@pytest.mark.parametrize("fmt", [E2M1, E4M3])
+def test_gradient_products_of_nan_groups(M, N, K, fmt):
+    """A group without a number reaches its 32 columns of the output and no others."""
+    codes, scales = random_operand(N, K, fmt, 7)
+    scales[N // 2, 3] = 255
+    dy = torch.full((M, N), 0.5, dtype=BF16, device=DEV)
+    out = torch.empty(M, K, dtype=BF16, device=DEV)
+    q.quest_grad_gemm_mx(0, dy, *on_device(codes, scales), fmt, M, N, K, out=out, workspace=grad_scratch(0, M, N, K))
+    assert bool(out[:, 96:128].isnan().all()) and not bool(out[:, :96].isnan().any()) and not bool(out[:, 128:].isnan().any())
 
 
 # ---- norm

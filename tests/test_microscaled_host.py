@@ -70,9 +70,11 @@ def test_gradient_products_refuse(lib):
     for missing in ("dy", "c", "s", "out"):
         assert call(**{missing: None}) == NULL
     assert call(which=2) == ARG and call(which=-1) == ARG and call(fmt=2) == DTYPE
-    assert call(M=64) == SHAPE and call(M=520) == SHAPE and call(which=1, N=64) == SHAPE and call(K=64) == SHAPE
+    assert call(M=520) == SHAPE and call(N=32) == SHAPE and call(K=96) == SHAPE and call(M=1 << 23) == SHAPE and call(M=-64) == SHAPE
     need = q.quest_grad_gemm_mx_workspace_bytes(0, 512, 256, 512)
-    assert need == 256 * 512 * 2 and q.quest_grad_gemm_mx_workspace_bytes(0, 64, 256, 512) == -1
+    assert need == 256 * 512 * 2 and q.quest_grad_gemm_mx_workspace_bytes(0, 64, 256, 512) == 0
+    assert q.quest_grad_gemm_mx_workspace_bytes(0, 96, 256, 512) == -1
+    assert call(M=0) == OK and call(which=1, N=0, ws=None, wsb=0) == OK
     assert q.quest_grad_gemm_mx_workspace_bytes(2, 512, 256, 512) == -1
     assert call(ws=None, wsb=0) == ARG and call(wsb=need - 1) == ARG and call(wsb=-1) == ARG
     assert call(dy=ODD) == ALIGN and call(c=ODD) == ALIGN and call(out=ODD) == ALIGN and call(ws=ODD) == ALIGN
