@@ -33,6 +33,38 @@ __device__ __forceinline__ float dpp_moved(float v)
 }
 constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E;   // quad_perm [1, 0, 3, 2] and [2, 3, 0, 1]
 
+// the value of the lane whose number differs in bit BIT: within rows of sixteen by lane patterns, beyond through the crossbar
+template <int BIT>
+__device__ __forceinline__ float lane_xor(float v)
+{
+    if constexpr (BIT == 1)
+        return dpp_moved<kDppXor1>(v);
+    else if constexpr (BIT == 2)
+        return dpp_moved<kDppXor2>(v);
+    else if constexpr (BIT == 4)
+        return dpp_moved<0x141>(dpp_moved<0x1B>(v));   // quad_perm [3, 2, 1, 0], then row_half_mirror
+    else if constexpr (BIT == 8)
+        return dpp_moved<0x128>(v);                     // row_ror:8
+    else
+        return __shfl_xor(v, BIT, kWave);
+}
+
+// The transform's strides that lie across lanes: N values to a lane, log2n of the block, FIRST = log2 N.  (An exact product:
+// a + b in the lower lane, a - b in the upper one.)
+template <int N, int FIRST>
+__device__ __forceinline__ void lane_butterflies(float (&v)[N], int log2n, int lane)
+{
+    static_for<6>([&](auto s) {
+        constexpr int bit = 1 << decltype(s)::value;
+        if (log2n > FIRST + decltype(s)::value) {
+            const float sign = (lane & bit) ? -1.0f : 1.0f;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                v[e] = __fmaf_rn(v[e], sign, lane_xor<bit>(v[e]));
+        }
+    });
+}
+
 // Block Hadamard transform of consecutive elements, eight to a lane, over 2^log2n elements (<= 512: 64 lanes), strides 1, 2, ..;
 // then the factor 2^(-log2n / 2).  (Strides in this order everywhere: the sums round the same whatever kernel a call takes.)
 __device__ __forceinline__ void wave_hadamard(float (&v)[8], int log2n, float norm, int lane)
@@ -40,25 +72,33 @@ __device__ __forceinline__ void wave_hadamard(float (&v)[8], int log2n, float no
     if (log2n == 0)
         return;
     butterflies8(v, log2n);
-    auto stage = [&](int bit, auto &&other) {   // partner: the lane that differs in `bit`
-        const float sign = (lane & bit) ? -1.0f : 1.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float o = other(v[e]);
-            v[e] = __fmaf_rn(v[e], sign, o);    // exact product: a + b in the low lane, a - b in the high one
-        }
-    };
-    if (log2n > 3)
-        stage(1, [](float x) { return dpp_moved<kDppXor1>(x); });
-    if (log2n > 4)
-        stage(2, [](float x) { return dpp_moved<kDppXor2>(x); });
-    for (int s = 5; s < log2n; ++s) {
-        const int bit = 1 << (s - 3);
-        stage(bit, [=](float x) { return __shfl_xor(x, bit, kWave); });
-    }
+    lane_butterflies<8, 3>(v, log2n, lane);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         v[e] *= norm;
+}
+
+// Eight elements in units of their scale to codes: nearest, ties to the even code, clipped at the largest element
+template <int FORMAT>
+__device__ __forceinline__ void mx_convert(float (&t)[8], uint32_t (&words)[MxFormat<FORMAT>::kWords])
+{
+    typedef MxFormat<FORMAT> F;
+    if constexpr (F::kE4M3) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            t[e] = __builtin_amdgcn_fmed3f(t[e], -F::kLargest, F::kLargest);   // (the conversion makes NaN of what lies beyond)
+        words[0] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
+        words[0] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], (int)words[0], true);
+        words[1] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[4], t[5], 0, false);
+        words[1] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[6], t[7], (int)words[1], true);
+    } else {
+        uint32_t w = 0;   // (the conversion clips)
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[0], t[1], 1.0f, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[2], t[3], 1.0f, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[4], t[5], 1.0f, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[6], t[7], 1.0f, 3);
+        words[0] = w;
+    }
 }
 
 // Eight elements of a group of 32 (the other 24 in the three neighbouring lanes) to codes, scale byte and trust bits
@@ -91,22 +131,7 @@ __device__ __forceinline__ MxEncoded<FORMAT> mx_encode(const float (&v)[8])
         t[e] = finite ? __fmul_rn(v[e], inverse) : 0.0f;
         out.trust |= (finite && fabsf(t[e]) <= F::kTrusted ? 1u : 0u) << e;
     }
-    if constexpr (F::kE4M3) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            t[e] = fminf(fmaxf(t[e], -F::kLargest), F::kLargest);   // (the conversion makes NaN of what lies beyond)
-        out.words[0] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
-        out.words[0] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], (int)out.words[0], true);
-        out.words[1] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[4], t[5], 0, false);
-        out.words[1] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[6], t[7], (int)out.words[1], true);
-    } else {
-        uint32_t w = 0;                                             // nearest, ties to even, clipped at 6
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[0], t[1], 1.0f, 0);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[2], t[3], 1.0f, 1);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[4], t[5], 1.0f, 2);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[6], t[7], 1.0f, 3);
-        out.words[0] = w;
-    }
+    mx_convert<FORMAT>(t, out.words);
     return out;
 }
 

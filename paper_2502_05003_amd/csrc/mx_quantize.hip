@@ -9,7 +9,8 @@ namespace quest {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnit = 512;   // elements of a wave: eight to a lane
+constexpr int kUnit = 512;              // elements of a wave with eight to a lane
+constexpr int kWaveBlock = 64 * 32;     // largest Hadamard block of a wave with 32 to a lane
 
 template <int FORMAT>
 __device__ __forceinline__ void store_encoded(const MxEncoded<FORMAT> &q, int64_t at, uint8_t *codes, uint8_t *scales,
@@ -25,12 +26,13 @@ __device__ __forceinline__ void store_encoded(const MxEncoded<FORMAT> &q, int64_
         mask[at / 8] = (uint8_t)q.trust;
 }
 
-// Blocks of up to 512 elements: a wave takes 512 consecutive elements, of one row or several (blocks divide rows, so units that
-// start at multiples of 512 cut none), and nothing leaves its registers in between.
+// Blocks of up to 512 elements: a wave takes 512 consecutive elements, of one row or several (blocks divide rows, so waves that
+// start at multiples of 512 elements cut none), eight to a lane.
 template <typename T, int FORMAT>
-__global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const T *__restrict__ x, int64_t elements, int cols, int64_t ld,
-                                                               int log2n, float norm, uint8_t *__restrict__ codes,
-                                                               uint8_t *__restrict__ scales, uint8_t *__restrict__ mask)
+__global__ __launch_bounds__(kThreads) void mx_quantize_lanes_kernel(const T *__restrict__ x, int64_t elements, int cols,
+                                                                     int64_t ld, int log2n, float norm,
+                                                                     uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
+                                                                     uint8_t *__restrict__ mask)
 {
     const int lane = threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -49,6 +51,113 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const T *__restri
     const MxEncoded<FORMAT> q = mx_encode<FORMAT>(v);
     if (at < elements)
         store_encoded<FORMAT>(q, at, codes, scales, mask, (lane & 3) == 0);
+}
+
+// Stages 1, 2, .. of the transform on 32 elements of a lane, then (blocks of 64 and more) across lanes; without the factor
+__device__ __forceinline__ void group_butterflies(float (&v)[32], int log2n, int lane)
+{
+#pragma unroll
+    for (int s = 0; s < 5; ++s) {
+        if (s < log2n) {
+            const int h = 1 << s;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                if ((i & h) == 0) {
+                    const float a = v[i], b = v[i + h];
+                    v[i] = a + b;
+                    v[i + h] = a - b;
+                }
+            }
+        }
+    }
+    lane_butterflies<32, 5>(v, log2n, lane);
+}
+
+/*
+ * Blocks of up to 2048 elements.  A lane takes a group of 32 elements as a whole, so that the first five strides of the
+ * transform, the group's maximum and its scale stay in the lane and are computed once: 10 vector instructions per element where
+ * eight elements to a lane take 19, which bound the kernel above in bf16.  A wave takes 64 consecutive groups; a lane's loads are 64
+ * (fp32: 128) bytes apart from its neighbour's, and each line is used up by them all, in the CU's cache.
+ * us, eight elements to a lane / so: 16384 x 2048 in bf16, blocks of 32, E2M1 with mask 26 / 18 (17 at the rate of a large copy);
+ * to E4M3 as it is 16.9 / 16.4; 24 x 5632, where the chip is empty, 2.1 / 2.8; 8192 x 4096 in fp32 29.5 / 34.  Blocks of 512 take
+ * 26 us, blocks of 2048 29 (through LDS, as the larger ones below, 44).
+ */
+template <typename T, int FORMAT>
+__global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const T *__restrict__ x, int64_t groups, int row_groups, int64_t ld,
+                                                               int log2n, float norm, uint8_t *__restrict__ codes,
+                                                               uint8_t *__restrict__ scales, uint8_t *__restrict__ mask)
+{
+    typedef MxFormat<FORMAT> F;
+    const int lane = threadIdx.x & 63;
+    const int64_t first = ((int64_t)blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kWave;
+    const int64_t g = first + lane;
+    float v[32] = {};
+    if (g < groups) {
+        int64_t from = g * kMxGroup;
+        if (ld != (int64_t)row_groups * kMxGroup) {   // the row the wave starts in by one division, the lane's by another, of a small number
+            const int64_t row = first / row_groups;
+            const int column = (int)(first - row * row_groups) + lane, more = column / row_groups;
+            from = (row + more) * ld + (int64_t)(column - more * row_groups) * kMxGroup;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float part[8];
+            load8(x + from + 8 * i, part);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[8 * i + e] = part[e];
+        }
+    }
+    group_butterflies(v, log2n, lane);
+
+    // largest magnitude (a NaN stays one); of the values with their factor, since rounding keeps the order
+    float top = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+        top = __builtin_elementwise_maximum(top, fabsf(v[e]));
+    const uint32_t largest = __float_as_uint(top * norm);
+    const int field = (int)(largest >> 23);
+    const bool finite = field < 255;   // (a NaN may carry a sign, which is above the field)
+    const uint32_t scale = finite ? (uint32_t)max(field - F::kMaxExponent, 0) : 255u;
+    if (__any(!finite)) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            v[e] = finite ? v[e] : 0.0f;
+    }
+    // t = x_h 2^-e in one product with norm 2^-e, which rounds like x_h = v norm does, as long as neither is subnormal
+    float factor = __uint_as_float((finite ? 254u - scale : 127u) << 23);
+    if (__any(largest != 0 && (scale < 32u || scale > 192u))) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            v[e] *= norm;
+    } else {
+        factor *= norm;
+    }
+    uint32_t untrusted = 0, words[4 * F::kWords];
+#pragma unroll
+    for (int i = 3; i >= 0; --i) {
+        float t[8];
+#pragma unroll
+        for (int e = 7; e >= 0; --e) {
+            t[e] = __fmul_rn(v[8 * i + e], factor);
+            // (the sign bit of what is left to the border, shifted in)
+            untrusted = __builtin_amdgcn_alignbit(untrusted, __float_as_uint(F::kTrusted - fabsf(t[e])), 31);
+        }
+        uint32_t part[F::kWords];
+        mx_convert<FORMAT>(t, part);
+#pragma unroll
+        for (int w = 0; w < F::kWords; ++w)
+            words[F::kWords * i + w] = part[w];
+    }
+    if (g >= groups)
+        return;
+#pragma unroll
+    for (int w = 0; w < F::kWords; ++w)
+        reinterpret_cast<uint4 *>(codes + g * (kMxGroup * F::kBits / 8))[w] =
+            make_uint4(words[4 * w], words[4 * w + 1], words[4 * w + 2], words[4 * w + 3]);
+    scales[g] = (uint8_t)scale;
+    if (mask)
+        reinterpret_cast<uint32_t *>(mask)[g] = finite ? ~untrusted : 0u;
 }
 
 // Larger blocks: a workgroup holds a row in LDS for the transform's wider strides.
@@ -118,9 +227,15 @@ hipError_t launch(const MxQuantizeArgs &a, hipStream_t stream)
 {
     const float norm = (float)(1.0 / sqrt((double)(int64_t(1) << a.log2n)));
     const T *x = static_cast<const T *>(a.x);
-    if ((1 << a.log2n) <= kUnit) {
-        hipLaunchKernelGGL((mx_quantize_kernel<T, FORMAT>), dim3(blocks_for(a.rows * a.cols)), dim3(kThreads), 0, stream, x,
-                           a.rows * a.cols, (int)a.cols, a.ld, a.log2n, norm, a.codes, a.scales, a.mask);
+    const int64_t elements = a.rows * a.cols, groups = elements / kMxGroup;
+    // groups to lanes: bf16, from four waves a compute unit on, and the blocks that only they hold
+    const bool whole = (1 << a.log2n) > kUnit || (sizeof(T) == 2 && groups >= 4 * 256 * kWave);
+    if ((1 << a.log2n) <= kWaveBlock && whole) {
+        hipLaunchKernelGGL((mx_quantize_kernel<T, FORMAT>), dim3((unsigned)((groups + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                           stream, x, groups, (int)(a.cols / kMxGroup), a.ld, a.log2n, norm, a.codes, a.scales, a.mask);
+    } else if ((1 << a.log2n) <= kUnit) {
+        hipLaunchKernelGGL((mx_quantize_lanes_kernel<T, FORMAT>), dim3(blocks_for(elements)), dim3(kThreads), 0, stream, x, elements,
+                           (int)a.cols, a.ld, a.log2n, norm, a.codes, a.scales, a.mask);
     } else {
         const hipError_t err = prepare_mx_quantize_kernels();
         if (err != hipSuccess)

@@ -66,7 +66,8 @@ def check_quantized(x, block, fmt, got):
 
 
 SHAPES = [(1, 32, 1), (1, 32, 32), (3, 96, 32), (3, 96, 16), (5, 640, 128), (777, 640, 2), (129, 512, 512), (64, 1280, 256),
-          (33, 5632, 1), (24, 5632, 512), (7, 2048, 1024), (2, 16384, 16384), (3, 5632, 8), (2, 2048, 4), (300, 4096, 64)]
+          (33, 5632, 1), (24, 5632, 512), (7, 2048, 1024), (2, 16384, 16384), (3, 5632, 8), (2, 2048, 4), (300, 4096, 64),
+          (5, 8192, 4096), (1100, 2080, 32), (1030, 2048, 2048), (3300, 640, 128), (520, 4128, 1), (4200, 512, 16)]
 
 
 @pytest.mark.parametrize("rows,cols,block", SHAPES)
@@ -81,15 +82,15 @@ def test_quantizer(rows, cols, block, fmt, dtype):
     assert np.all(np.abs(xh - exact) <= 1e-5 * np.maximum(np.abs(exact), np.sqrt((exact ** 2).mean(-1, keepdims=True))))
 
 
-@pytest.mark.parametrize("block,ld", [(32, 176), (16, 168), (1024, 2056)])
+@pytest.mark.parametrize("rows,cols,block,ld", [(37, 160, 32, 176), (37, 160, 16, 168), (37, 2048, 1024, 2056), (9, 4096, 4096, 4104),
+                                                (14000, 160, 32, 176), (1100, 2080, 4, 2096)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
-def test_quantizer_strided_rows_without_a_mask(block, ld, dtype):
-    cols = 160 if block < 160 else 2048
-    x = rows_of(37, ld, dtype, 3)[:, :cols]
-    got = buffers(37, cols, E2M1, mask=False)
-    q.quest_hadamard_quantize_mx(x.to(DEV)[:, :], block, E2M1, **got)
-    wide = rows_of(37, ld, dtype, 3).to(DEV)
-    again = buffers(37, cols, E2M1, mask=False)
+def test_quantizer_strided_rows_without_a_mask(rows, cols, block, ld, dtype):
+    x = rows_of(rows, ld, dtype, 3)[:, :cols]
+    got = buffers(rows, cols, E2M1, mask=False)
+    q.quest_hadamard_quantize_mx(x.contiguous().to(DEV), block, E2M1, **got)
+    wide = rows_of(rows, ld, dtype, 3).to(DEV)
+    again = buffers(rows, cols, E2M1, mask=False)
     q.quest_hadamard_quantize_mx(wide[:, :cols], block, E2M1, **again)
     check_quantized(x, block, E2M1, again)
     assert torch.equal(got["codes"], again["codes"]) and torch.equal(got["scales"], again["scales"])
@@ -124,6 +125,13 @@ def test_quantizer_borders(fmt):
     got = buffers(1, x.shape[1], fmt)
     q.quest_hadamard_quantize_mx(x.to(DEV), 1, fmt, **got)
     check_quantized(x, 1, fmt, got)
+    # in bf16 (where all points but those next to a tie are exact), a row often enough for every kernel, with and without a transform
+    many = x.to(BF16).expand(70000 // x.shape[1] * 32 + 1, -1).contiguous()
+    for block in (1, 32):
+        got = buffers(*many.shape, fmt)
+        q.quest_hadamard_quantize_mx(many.to(DEV), block, fmt, **got)
+        with np.errstate(invalid="ignore", over="ignore"):
+            check_quantized(many, block, fmt, got)
 
 
 def test_quantizer_leaves_what_is_behind_its_outputs():
