@@ -25,6 +25,23 @@ __device__ __forceinline__ float block_sum(float v, float *park)
     return sum;
 }
 
+/*
+ * 1 / sqrt(sum * share + eps), rounded once: the fp32 value of four roundings takes one Newton step in 64 bits, since a row's every
+ * element carries its error, and with it the codes that lie next to a rounding's edge.  (A step with t = m r, r += r (1 - t r) / 2,
+ * squares the error.)  Nothing for 0, NaN for what fp32 does not hold.
+ */
+__device__ __forceinline__ float reciprocal_root(float sum, double share, float eps)
+{
+    const double m = __fma_rn((double)sum, share, (double)eps);
+    const float mean = (float)m;
+    if (mean == 0.0f)
+        return 0.0f;
+    if (!(mean < INFINITY))
+        return NAN;
+    const double r = 1.0f / sqrtf(mean);
+    return (float)__fma_rn(0.5 * r, __fma_rn(-m * r, r, 1.0), r);
+}
+
 // eight elements rounded to the type (bf16: by the hardware's conversion)
 __device__ __forceinline__ void store8_packed(float *p, const float (&v)[8]) { store8(p, v); }
 __device__ __forceinline__ void store8_packed(uint16_t *p, const float (&v)[8])
@@ -47,7 +64,7 @@ __global__ __launch_bounds__(kThreads) void rms_norm_kernel(const T *__restrict_
     __shared__ float park[kWaves];
     const int64_t row = blockIdx.x, first = row * cols;
     const int lane = threadIdx.x & 63;
-    float v[CH][8], sum = 0.0f;
+    float v[CH][8], w[CH][8], sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = (i * kThreads + threadIdx.x) * 8;
@@ -57,6 +74,7 @@ __global__ __launch_bounds__(kThreads) void rms_norm_kernel(const T *__restrict_
         if (c >= cols)
             continue;
         load8(x + row * ld_x + c, v[i]);
+        load8(weight + c, w[i]);   // here, so that the sum does not stand between the call's two trips to memory
         if (residual) {
             float r[8];
             load8(residual + row * ld_residual + c, r);
@@ -69,19 +87,16 @@ __global__ __launch_bounds__(kThreads) void rms_norm_kernel(const T *__restrict_
         for (int e = 0; e < 8; ++e)
             sum = __fmaf_rn(v[i][e], v[i][e], sum);
     }
-    const float mean = block_sum<kWaves>(sum, park) / (float)cols + eps;
-    const float rstd = mean == 0.0f ? 0.0f : mean < INFINITY ? 1.0f / sqrtf(mean) : NAN;
+    const float rstd = reciprocal_root(block_sum<kWaves>(sum, park), 1.0 / cols, eps);
     if (rstd_out && threadIdx.x == 0)
         rstd_out[row] = rstd;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = (i * kThreads + threadIdx.x) * 8;
         if (c < cols) {
-            float w[8];
-            load8(weight + c, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                v[i][e] = __fmul_rn(__fmul_rn(v[i][e], rstd), w[e]);
+                v[i][e] = __fmul_rn(__fmul_rn(v[i][e], rstd), w[i][e]);
             if (y_out)
                 store8_packed(y_out + first + c, v[i]);
         }
