@@ -9,9 +9,9 @@ namespace quest {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kRowThreads = 1024;   // most for a row's workgroup of the forward pass
 
-template <int WAVES>
-__device__ __forceinline__ float block_sum(float v, float *park)
+__device__ __forceinline__ float block_sum(float v, float *park, int waves)
 {
     v = wave_sum_dpp(v);
     __syncthreads();   // the numbers of the row before have been read
@@ -20,7 +20,7 @@ __device__ __forceinline__ float block_sum(float v, float *park)
     __syncthreads();
     float sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w)
+    for (int w = 0; w < waves; ++w)
         sum += park[w];
     return sum;
 }
@@ -53,21 +53,28 @@ __device__ __forceinline__ void store8_packed(uint16_t *p, const float (&v)[8])
 __device__ __forceinline__ float rounded(float v, const float *) { return v; }
 __device__ __forceinline__ float rounded(float v, const uint16_t *) { return bf16_bits_to_float(float_to_bf16_bits(v)); }
 
-// Thread t holds the elements 8 t + 2048 i .. + 8, i < CH: a wave's lanes hold 512 consecutive ones.
+/*
+ * Forward pass.  Bound by memory: x and residual are read, h, codes and scales written (16384 x 2048 in bf16, E4M3, 236 MB, 46 us at
+ * the rate of a large copy; it takes 47).  A row has a workgroup of its own, with as many waves as it needs: thread t of n holds
+ * the elements 8 (t + n i) .. + 8, i < CH, so that a wave's lanes hold 512 consecutive ones.  Two chunks to a lane where a row has
+ * more than 512 elements.  (us for 2^25 elements in bf16 with four waves for each row / one chunk / two: rows of 512 109 / 49 / 50,
+ * 640 97 / 65 / 58, 1024 65 / 49 / 47, 2048 47 / 48 / 48, 4608 61 / 55 / 52, 11008 71 / - / 56)
+ */
 template <typename T, typename W, int CH, int FORMAT>
-__global__ __launch_bounds__(kThreads) void rms_norm_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ residual,
+__global__ __launch_bounds__(kRowThreads) void rms_norm_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ residual,
                                                             int64_t ld_residual, const W *__restrict__ weight, int cols, float eps,
                                                             T *__restrict__ h_out, T *__restrict__ y_out, int log2n, float norm,
                                                             uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
                                                             uint8_t *__restrict__ mask, float *__restrict__ rstd_out)
 {
-    __shared__ float park[kWaves];
+    __shared__ float park[kRowThreads / kWave];
+    const int threads = blockDim.x;
     const int64_t row = blockIdx.x, first = row * cols;
     const int lane = threadIdx.x & 63;
     float v[CH][8], w[CH][8], sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = (i * kThreads + threadIdx.x) * 8;
+        const int c = (i * threads + threadIdx.x) * 8;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             v[i][e] = 0.0f;
@@ -87,12 +94,12 @@ __global__ __launch_bounds__(kThreads) void rms_norm_kernel(const T *__restrict_
         for (int e = 0; e < 8; ++e)
             sum = __fmaf_rn(v[i][e], v[i][e], sum);
     }
-    const float rstd = reciprocal_root(block_sum<kWaves>(sum, park), 1.0 / cols, eps);
+    const float rstd = reciprocal_root(block_sum(sum, park, threads / kWave), 1.0 / cols, eps);
     if (rstd_out && threadIdx.x == 0)
         rstd_out[row] = rstd;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = (i * kThreads + threadIdx.x) * 8;
+        const int c = (i * threads + threadIdx.x) * 8;
         if (c < cols) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -222,7 +229,7 @@ __global__ __launch_bounds__(backward_threads(GROUP)) void rms_norm_backward_ker
                 }
             }
         }
-        const float mean = (GROUP == 1 ? wave_sum_dpp(sum) : block_sum<GROUP>(sum, park)) / (float)cols;
+        const float mean = (GROUP == 1 ? wave_sum_dpp(sum) : block_sum(sum, park, GROUP)) / (float)cols;
         if (mine) {
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
@@ -298,31 +305,22 @@ int parts_of(int64_t rows, int64_t cols)
     return (int)std::min<int64_t>((rows + groups_of(cols) - 1) / groups_of(cols), 512);
 }
 
-// f(std::integral_constant<int, CH>) for the number of chunks of 2048 elements that a row has
-template <typename F>
-void with_chunks(int64_t cols, F &&f)
-{
-    if (cols <= 2048)
-        f(std::integral_constant<int, 1>());
-    else if (cols <= 4096)
-        f(std::integral_constant<int, 2>());
-    else if (cols <= 8192)
-        f(std::integral_constant<int, 4>());
-    else
-        f(std::integral_constant<int, 8>());
-}
-
 template <typename T, typename W>
 hipError_t launch_forward(const RmsNormArgs &a, hipStream_t stream)
 {
-    with_chunks(a.cols, [&](auto ch) {
-        auto kernel = a.format == QUEST_MX_E4M3 ? rms_norm_kernel<T, W, decltype(ch)::value, QUEST_MX_E4M3>
-                                                : rms_norm_kernel<T, W, decltype(ch)::value, QUEST_MX_E2M1>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, static_cast<const T *>(a.x), a.ld_x,
+    auto launch = [&](auto ch) {
+        constexpr int CH = decltype(ch)::value;
+        auto kernel = a.format == QUEST_MX_E4M3 ? rms_norm_kernel<T, W, CH, QUEST_MX_E4M3> : rms_norm_kernel<T, W, CH, QUEST_MX_E2M1>;
+        const unsigned threads = (unsigned)((a.cols + 8 * CH * kWave - 1) / (8 * CH * kWave) * kWave);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)a.rows), dim3(threads), 0, stream, static_cast<const T *>(a.x), a.ld_x,
                            static_cast<const T *>(a.residual), a.ld_residual, static_cast<const W *>(a.weight), (int)a.cols, a.eps,
                            static_cast<T *>(a.h_out), static_cast<T *>(a.y_out), a.log2n,
                            (float)(1.0 / sqrt((double)(int64_t(1) << a.log2n))), a.codes, a.scales, a.mask, a.rstd);
-    });
+    };
+    if (a.cols <= 8 * kWave)
+        launch(std::integral_constant<int, 1>());
+    else
+        launch(std::integral_constant<int, 2>());
     return hipGetLastError();
 }
 
