@@ -366,8 +366,8 @@ quest_status quest_lowbit_gemm_mx(const uint8_t *a_codes, const uint8_t *a_scale
  * quest_grad_gemm for microscaled operands of either format: the code-packed operand's value is bf16(v * 2^(scale - 127)).
  *   which = 0:  out[M, K] = dy[M, N] * what_h[N, K]      (q = weights [N, K])
  *   which = 1:  out[N, K] = dy[M, N]^T * xhat_h[M, K]    (q = activations [M, K])
- * M, N, K multiples of 64, each at most 2^22.  Workspace as for quest_grad_gemm, sized by quest_grad_gemm_mx_workspace_bytes
- * (either format).
+ * M, N, K multiples of 64, each at most 2^22; an output of no elements is a no-op, a sum over nothing (which = 0: N = 0,
+ * which = 1: M = 0) gives zeros.  Workspace as for quest_grad_gemm, sized by quest_grad_gemm_mx_workspace_bytes (either format).
  */
 quest_status quest_grad_gemm_mx(int32_t which, const void *dy, const uint8_t *q_codes, const uint8_t *q_scales,
                                 quest_mx_format q_format, int64_t M, int64_t N, int64_t K, void *out, void *workspace,

@@ -177,6 +177,14 @@ __global__ __launch_bounds__(256) void expand_mx_codes_kernel(const uint8_t *__r
     }
 }
 
+// What a product over nothing is: zeros, eight of them to a thread
+__global__ __launch_bounds__(256) void grad_zeros_kernel(uint4 *__restrict__ out, uint32_t count)
+{
+    const uint32_t at = blockIdx.x * 256u + threadIdx.x;
+    if (at < count)
+        out[at] = make_uint4(0, 0, 0, 0);
+}
+
 // Work is counted in (tile, step) units: tile t owns the units [t * steps, (t + 1) * steps) and
 // workgroup b (in XCD-major order) the units [b * per_block, (b + 1) * per_block).  With
 // per_block = steps every workgroup computes one whole tile.  When the tiles do not fill the CUs
@@ -869,6 +877,19 @@ hipError_t prepare_grad_gemm_kernels()
             err = prepare_mode<2>();
         return err;
     });
+}
+
+hipError_t launch_grad_zeros(void *out, int64_t rows, int64_t cols, hipStream_t stream)
+{
+    auto *at = static_cast<uint4 *>(out);
+    constexpr int64_t kLaunch = int64_t(1) << 30;   // 16-byte pieces of a launch
+    hipError_t err = hipSuccess;
+    for (int64_t left = rows * cols / 8; left > 0 && err == hipSuccess; left -= kLaunch, at += kLaunch) {
+        const uint32_t count = (uint32_t)std::min(left, kLaunch);
+        hipLaunchKernelGGL(grad_zeros_kernel, dim3((count + 255) / 256), dim3(256), 0, stream, at, count);
+        err = hipGetLastError();
+    }
+    return err;
 }
 
 hipError_t launch_grad_gemm(const GradGemmArgs &a, hipStream_t stream)

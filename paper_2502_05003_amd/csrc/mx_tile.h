@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
     auto transfer = [&](auto pc, uint32_t stage, int at, bool half) __attribute__((always_inline)) {
         constexpr int p = decltype(pc)::value, h = p & 1, q = p - nA;
         const uint32_t less = !kE4M3 && half ? back[h] : 0u;
-        // (M0 for four at a time: the others differ in the instruction's offset, which moves both ends; rows are 256 bytes or more
+        // (M0 for four at a time: the others differ in the instruction's offset, which moves both ends; rows are 128 bytes or more
         // apart, so the offset in memory that makes up for it is not negative)
         if constexpr (p < nA) {
             constexpr int more = 1024 * (p % 4);
@@ -205,8 +205,9 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
     };
     const uint32_t scale_at = (uint32_t)lane * (uint32_t)row_scales;
     const uint32_t scale_addr = smem_addr + 2 * T::kStage;
-    // first scale dword of the 16 bytes that hold a stage's (the last ones of a row end where the row ends)
-    auto chunk_start = [&](int at) { return min(at * T::kStageK / kScaleChunk * 4, words - 4); };
+    // first scale dword of the 16 bytes that hold a stage's (the last ones of a row end where the row ends; a row of three is
+    // followed by something that no stage uses)
+    auto chunk_start = [&](int at) { return max(min(at * T::kStageK / kScaleChunk * 4, words - 4), 0); };
     auto transfer_scales = [&](int buffer, int at) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < (WI + WJ + 3) / 4; ++h) {
@@ -471,7 +472,7 @@ hipError_t launch_tiles(const MxGemmArgs &a, hipStream_t stream)
     const bool pieces_fit = a.y && !a.acc_out && (a.ld_y & 7) == 0 && (a.N & 7) == 0 && a.ld_y < (1 << 24) &&
                             (reinterpret_cast<uintptr_t>(a.y) & 15) == 0;
     auto kernel = pieces_fit ? mx_tile_kernel<FORMAT, WI, WJ, false, false> : mx_tile_kernel<FORMAT, WI, WJ, false, true>;
-    if constexpr (!T::kE4M3) {   // (in E4M3 the shortest contraction has four)
+    if constexpr (!T::kE4M3) {   // (in E4M3 the shortest contraction has three)
         if (a.K <= 2 * T::kStageK)
             kernel = pieces_fit ? mx_tile_kernel<FORMAT, WI, WJ, true, false> : mx_tile_kernel<FORMAT, WI, WJ, true, true>;
     }
@@ -498,7 +499,7 @@ hipError_t prepare_tiles()
     return err;
 }
 
-// a.M, a.N of any size, a.K >= kScaleChunk; tiles of `block` x `block`: 256 or 128
+// a.M, a.N of any size, a.K >= 384, which are two stages or more; tiles of `block` x `block`: 256 or 128
 template <int FORMAT>
 hipError_t launch_mx_tiles(const MxGemmArgs &a, int block, hipStream_t stream)
 {

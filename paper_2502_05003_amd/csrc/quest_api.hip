@@ -630,7 +630,7 @@ namespace {
 quest_status mx_shape_checks(int64_t rows, int64_t cols, int64_t had_block, int64_t largest_block, int *log2n)
 {
     if (rows < 0 || cols < QUEST_MX_GROUP || cols > QUEST_MAX_COLS || (cols % QUEST_MX_GROUP) || rows > QUEST_MAX_MX_ROWS ||
-        rows * cols > (int64_t(1) << 34))   // (a launch has fewer than 2^32 threads: eight elements each, or 256 for a row)
+        rows * cols > (int64_t(1) << 34))   // (a launch has fewer than 2^32 threads: one for eight elements, or a wave or more for a row)
         return QUEST_ERR_SHAPE;
     const int l = exact_log2(had_block);
     if (l < 0 || had_block > largest_block || cols % had_block)
@@ -730,7 +730,9 @@ quest_status quest_grad_gemm_mx(int32_t which, const void *dy, const uint8_t *q_
 {
     if (which != 0 && which != 1)
         return QUEST_ERR_ARG;
-    if (!dy || !q_codes || !q_scales || !out)
+    const int64_t inner = which == 0 ? N : M, out_rows = which == 0 ? M : N;
+    const bool empty = out_rows == 0 || K == 0;
+    if (!empty && (!out || (inner != 0 && (!dy || !q_codes || !q_scales))))
         return QUEST_ERR_NULL;
     if (!known_format(q_format))
         return QUEST_ERR_DTYPE;
@@ -741,6 +743,10 @@ quest_status quest_grad_gemm_mx(int32_t which, const void *dy, const uint8_t *q_
         return QUEST_ERR_ALIGN;
     if (workspace_bytes < 0 || (needed > 0 && (!workspace || workspace_bytes < needed)))
         return QUEST_ERR_ARG;
+    if (empty)
+        return QUEST_OK;
+    if (inner == 0)
+        return launched(quest::launch_grad_zeros(out, out_rows, K, static_cast<hipStream_t>(stream)));
 
     quest::GradGemmArgs args;
     args.which = which;

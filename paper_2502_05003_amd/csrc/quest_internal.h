@@ -232,6 +232,7 @@ double grad_gemm_mid_cost(int grid, int64_t C, int64_t R, int64_t K, int cus);
 
 // hipErrorInvalidValue: the shape is not one the kernels cover, or the workspace is too small
 // (the entry points check both beforehand with grad_gemm_workspace_bytes).
+hipError_t launch_grad_zeros(void *out, int64_t rows, int64_t cols, hipStream_t stream);   // bf16, whole 16-byte pieces
 hipError_t launch_grad_gemm(const GradGemmArgs &a, hipStream_t stream);
 // Scratch bytes a call with these arguments needs on a device with `cus` compute units (0 for the
 // small-shape kernel, which dequantizes in place); -1 when no kernel covers the shape.

@@ -195,7 +195,10 @@ def product_bound(a, b, fmt):
 
 PRODUCTS = [(1, 1, 128), (1, 5632, 2048), (7, 33, 384), (16, 640, 5632), (24, 96, 1024), (65, 130, 256), (130, 257, 128),
             (333, 512, 1024), (300, 1283, 640), (1030, 520, 512), (32, 4096, 256), (200, 1024, 384), (256, 2040, 256), (300, 2100, 384),
-            (40, 9000, 512)]
+            (40, 9000, 512), (300, 2100, 256), (24, 9000, 512)]
+# every block of few rows with units of 128 that groups of two and of four do and do not divide
+PRODUCTS += [(M, N, K) for M, N in ((5, 40), (13, 4200)) for K in (1152, 2048, 2176, 2304, 2432)]
+PRODUCTS += [(M, N, K) for M, N in ((29, 8300), (125, 4003)) for K in (1152, 2432)] + [(128, 8000, 1152), (66, 8130, 2432)]
 
 
 @pytest.mark.parametrize("M,N,K", PRODUCTS)
@@ -226,7 +229,7 @@ def sampled(count, rng):
 
 
 LARGE_PRODUCTS = [(2100, 2200, 512), (2100, 2200, 640), (2303, 2056, 1152), (4097, 1288, 2048), (1800, 5128, 768), (2600, 4104, 512),
-                  (2600, 4104, 640), (6000, 4104, 1152)]
+                  (2600, 4104, 640), (6000, 4104, 1152), (2100, 2200, 384), (6000, 8205, 384)]
 
 
 @pytest.mark.parametrize("M,N,K", LARGE_PRODUCTS)
@@ -355,6 +358,17 @@ def test_gradient_products_of_nan_groups(M, N, K, fmt):
     out = torch.empty(M, K, dtype=BF16, device=DEV)
     q.quest_grad_gemm_mx(0, dy, *on_device(codes, scales), fmt, M, N, K, out=out, workspace=grad_scratch(0, M, N, K))
     assert bool(out[:, 96:128].isnan().all()) and not bool(out[:, :96].isnan().any()) and not bool(out[:, 128:].isnan().any())
+
+
+@pytest.mark.parametrize("which,M,N,K", [(0, 128, 0, 192), (1, 0, 320, 64), (0, 0, 128, 192), (1, 64, 0, 128)])
+@pytest.mark.parametrize("fmt", [E2M1, E4M3])
+def test_gradient_products_over_nothing(which, M, N, K, fmt):
+    """No tokens, or no outputs that a gradient reached: zeros, not what was there; an output of no elements is left alone."""
+    rows, width = (M if which else N), K if fmt == E4M3 else K // 2
+    codes, scales = torch.empty(rows, width, dtype=torch.uint8, device=DEV), torch.empty(rows, K // 32, dtype=torch.uint8, device=DEV)
+    out = torch.full((N if which else M, K), float("nan"), dtype=BF16, device=DEV)
+    q.quest_grad_gemm_mx(which, torch.empty(M, N, dtype=BF16, device=DEV), codes, scales, fmt, M, N, K, out=out)
+    assert bool((out == 0).all())
 
 
 # ---- norm
@@ -576,6 +590,38 @@ def test_captured_step_on_another_stream():
         torch.cuda.synchronize()
         for k, v in {**t, **xq}.items():
             assert torch.equal(v, expected[k]), k
+
+
+@pytest.mark.parametrize("M,N,K,fmt", [(2100, 2057, 640, E2M1), (2304, 4096, 512, E4M3), (40, 9000, 384, E2M1), (3, 640, 2048, E4M3)])
+def test_captured_products_of_two_streams(M, N, K, fmt):
+    """Two captured graphs of products, replayed at once on two streams, with eager calls between."""
+    q.quest_init()
+    streams, graphs, ys, operands = [torch.cuda.Stream() for _ in range(2)], [], [], []
+    for i, stream in enumerate(streams):
+        operands.append(on_device(*random_operand(M, K, fmt, i)) + on_device(*random_operand(N, K, E2M1, i + 2)))
+        ys.append(torch.empty(M, N, dtype=BF16, device=DEV))
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            a, sa, b, sb = operands[i]
+            q.quest_lowbit_gemm_mx(a, sa, fmt, b, sb, K, y=ys[i])
+        graphs.append(graph)
+    for seed in (10, 20, 30):
+        expected = []
+        for i in range(2):
+            for mine, new in zip(operands[i], random_operand(M, K, fmt, seed + i) + random_operand(N, K, E2M1, seed + i + 2)):
+                mine.copy_(torch.from_numpy(new))
+            a, sa, b, sb = operands[i]
+            expected.append(torch.empty_like(ys[i]))
+            q.quest_lowbit_gemm_mx(a, sa, fmt, b, sb, K, y=expected[i])
+            ys[i].zero_()
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for y, ref in zip(ys, expected):
+            assert torch.equal(y, ref)
 
 
 def test_decoding_step():

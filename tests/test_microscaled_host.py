@@ -2,6 +2,8 @@
 definitions that the GPU tests compare with."""
 import ctypes
 import inspect
+import os
+import subprocess
 import types
 
 import numpy as np
@@ -10,6 +12,9 @@ import torch
 
 from oracle import microscaled as mx
 from paper_2502_05003_amd import binding as q
+from paper_2502_05003_amd import build
+
+from test_kernel_ordering import reads_outstanding_at_barriers
 
 FAKE, ODD = ctypes.c_void_p(0x10000), ctypes.c_void_p(0x10008)   # never dereferenced: validation fails first, or nothing to do
 OFF1, OFF2 = ctypes.c_void_p(0x10001), ctypes.c_void_p(0x10002)
@@ -75,9 +80,22 @@ def test_gradient_products_refuse(lib):
     assert need == 256 * 512 * 2 and q.quest_grad_gemm_mx_workspace_bytes(0, 64, 256, 512) == 0
     assert q.quest_grad_gemm_mx_workspace_bytes(0, 96, 256, 512) == -1
     assert call(M=0) == OK and call(which=1, N=0, ws=None, wsb=0) == OK
+    assert call(M=0, dy=None, out=None) == OK and call(which=1, N=0, dy=None, out=None, ws=None, wsb=0) == OK
+    assert call(N=0, out=None) == NULL and call(which=1, M=0, out=None) == NULL      # a sum over nothing is written, too
     assert q.quest_grad_gemm_mx_workspace_bytes(2, 512, 256, 512) == -1
     assert call(ws=None, wsb=0) == ARG and call(wsb=need - 1) == ARG and call(wsb=-1) == ARG
     assert call(dy=ODD) == ALIGN and call(c=ODD) == ALIGN and call(out=ODD) == ALIGN and call(ws=ODD) == ALIGN
+
+
+@pytest.mark.parametrize("source", ["mx_tiles_e2m1.hip", "mx_tiles_e4m3.hip"])
+def test_tiles_have_their_reads_back_at_barriers(source, tmp_path):
+    """The transfers behind a barrier refill the stage that was read ahead of it, so no wave may arrive with LDS reads on their way."""
+    out = tmp_path / "kernels.s"
+    subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), *build.HIPCC_FLAGS, *build.EXTRA_FLAGS.get(source, []),
+                    "--cuda-device-only", "-S", os.path.join(build.CSRC, source), "-o", str(out)], check=True, capture_output=True)
+    found = {k: v for k, v in reads_outstanding_at_barriers(out.read_text()).items() if "mx_tile_kernel" in k}
+    assert len(found) >= 4 and all(len(v) >= 3 for v in found.values())
+    assert {k: v for k, v in found.items() if any(v)} == {}
 
 
 def test_norm_refuses(lib):
@@ -367,6 +385,6 @@ def test_products_reach_every_kernel():
     for block in (128, 256):        # with workgroups that go on to another tile, and contractions of two stages, of whole ones and a half
         of = [s for s in gpu.LARGE_PRODUCTS if mx_plan(*s)[1] == block]
         assert any(-(-M // block) * -(-N // block) > 256 for M, N, K in of)
-        assert {K % 256 for M, N, K in of} == {0, 128} and 512 in {K for M, N, K in of}
-    assert mx_plan(1, 1 << 22, 65536)[0] == "few" and mx_plan(1 << 22, 1 << 22, 384) == ("few", 64, 64)
-    assert mx_plan(1 << 22, 1 << 22, 512) == ("tiles", 256, 256)
+        assert {K % 256 for M, N, K in of} == {0, 128} and {384, 512} <= {K for M, N, K in of}
+    assert mx_plan(1, 1 << 22, 65536)[0] == "few" and mx_plan(1 << 22, 1 << 22, 256) == ("few", 64, 64)
+    assert mx_plan(1 << 22, 1 << 22, 384) == ("tiles", 256, 256)
