@@ -11,7 +11,9 @@
 //   wait for the reads of block WI - 1 and for the next stage's transfers, which the first phases have issued; barrier
 // Nothing but the waits for these two interrupts the matrix instructions, tile ends included: the transfers run on into the
 // workgroup's next tile, whose first products start from zero (C = 0, no accumulator is cleared), and block b of a finished
-// tile is rounded, parked in the wave's corner of LDS and stored as whole row segments while block b + 1 is multiplied.
+// tile is rounded, parked in the wave's corner of LDS and stored as whole row segments while block b + 1 is multiplied.  The stores
+// are issued behind their stage's transfers and counted, so that nothing waits for them before the end of the stage that follows
+// (16384 x 5632 x 2048 132 -> 124 us, 16384 x 4096 x 1024 67 -> 62).
 //
 // What bounds it: with large contractions the chip's power (4096 x 4096 x 16640 in E2M1 139 us or 4.0 PFLOP/s; with operands of
 // zeros 103, and the matrix instructions alone, from registers, sustain 6.5), with short ones the tiles' ends on top (16384 x 5632
@@ -366,8 +368,17 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
                 }
             });
         };
-        // transfers spread over phases 1 and 2, in E2M1, which has more of them, over 3 (4096 x 4096 x 16640: 143 -> 139 us)
-        constexpr int kDmaPhases = kE4M3 || WI < 4 ? 2 : 3, kDmaSlots = kDmaPhases * kFragB;
+        // transfers spread over phases 1 and 2, in E2M1, which has more of them, over 3 (4096 x 4096 x 16640: 143 -> 139 us);
+        // where a tile before ends, all of them ahead of its stores
+        constexpr int kDmaSlots = boundary ? 5 * kFragB / kOutParts + 1 : (kE4M3 || WI < 4 ? 2 : 3) * kFragB;
+        constexpr int kStoresBehind = [] {   // the last of them
+            int count = 0;
+            for (int number = boundary ? 0 : 2; number < (boundary ? 2 : last ? WI : 0); ++number)
+                for (int piece = 0; piece < WJ / 2; ++piece)
+                    if (number * kFragB + (6 * piece + 5) * kFragB / kOutParts >= (kDma - 1) * kDmaSlots / kDma)
+                        count += 4;
+            return count;
+        }();
         auto phase = [&](auto blockc, auto numberc) __attribute__((always_inline)) {
             constexpr int block = decltype(blockc)::value, number = decltype(numberc)::value;   // number: 0 = phase 1
             constexpr bool before = number == 0;
@@ -389,7 +400,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
                     if constexpr (decltype(c)::value / 2 == f)
                         read_a(stage, std::integral_constant<int, next>{}, c);
                 });
-                if constexpr (number < kDmaPhases)
+                if constexpr (number * kFragB + f < kDmaSlots)
                     static_for<kDma>([&](auto p) {
                         if constexpr (decltype(p)::value * kDmaSlots / kDma == number * kFragB + f)
                             transfer(p, refill, fetched, fetched_half);
@@ -410,9 +421,10 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
         };
         phase(std::integral_constant<int, WI - 1>{}, std::integral_constant<int, 0>{});
         static_for<WI - 1>([&](auto i) { phase(i, std::integral_constant<int, decltype(i)::value + 1>{}); });
-        // the reads of block WI - 1 are back, the next stage has landed
+        // The reads of block WI - 1 are back, the next stage has landed.  Stores, which were issued behind its transfers, may be on
+        // their way until the stage behind it has landed.
         __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
-        wait_vmcnt<0>();
+        wait_vmcnt<GENERAL ? 0 : kStoresBehind>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");        // no read of the new stage ahead of it
         cur ^= 1;

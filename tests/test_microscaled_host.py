@@ -3,6 +3,7 @@ definitions that the GPU tests compare with."""
 import ctypes
 import inspect
 import os
+import re
 import subprocess
 import types
 
@@ -96,6 +97,50 @@ def test_tiles_have_their_reads_back_at_barriers(source, tmp_path):
     found = {k: v for k, v in reads_outstanding_at_barriers(out.read_text()).items() if "mx_tile_kernel" in k}
     assert len(found) >= 4 and all(len(v) >= 3 for v in found.values())
     assert {k: v for k, v in found.items() if any(v)} == {}
+    counted = 0
+    for kernel, waits in waits_at_barriers(out.read_text()).items():
+        if "mx_tile_kernel" in kernel:
+            assert all(allowed is not None and allowed <= stores for allowed, stores in waits), kernel
+            counted += sum(allowed > 0 for allowed, _ in waits)
+    assert counted >= 3      # tiles of 256: where one begins and where one ends; of 128: where one begins
+
+
+def waits_at_barriers(assembly):
+    """{kernel: [(memory operations that the last wait ahead of a barrier leaves on their way, stores between it and the last
+    transfer into LDS ahead of it)]}: with as many stores behind the transfers as are left, the transfers have landed."""
+    found, kernel, stores, last = {}, None, 0, None
+    for line in assembly.splitlines():
+        line = line.split(";")[0].strip()
+        label = re.match(r"(_Z\w+):", line)
+        if label:
+            kernel, stores, last = label.group(1), 0, None
+            found[kernel] = []
+        elif line.startswith("buffer_load") and line.endswith("lds"):
+            stores, last = 0, None
+        elif line.startswith("buffer_store"):
+            stores += 1
+        elif line.startswith("s_waitcnt"):
+            wait = re.search(r"vmcnt\((\d+)\)", line)
+            if wait and (last is None or int(wait.group(1)) <= last[0]):
+                last = (int(wait.group(1)), stores)
+        elif line.startswith("s_barrier"):
+            found[kernel].append(last or (None, stores))
+            last = None
+    return found
+
+
+def test_the_waits_on_a_sample():
+    sample = """
+_Zk:
+	buffer_load_dwordx4 v1, s[0:3], 0 offen lds
+	buffer_store_dwordx4 v[2:5], v6, s[4:7], 0 offen
+	s_waitcnt vmcnt(1)
+	s_barrier
+	buffer_load_dwordx4 v1, s[0:3], 0 offen offset:1024 lds
+	s_waitcnt lgkmcnt(0)
+	s_barrier
+"""
+    assert waits_at_barriers(sample) == {"_Zk": [(1, 1), (None, 0)]}
 
 
 def test_norm_refuses(lib):
