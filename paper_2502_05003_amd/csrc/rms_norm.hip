@@ -11,10 +11,12 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kRowThreads = 1024;   // most for a row's workgroup of the forward pass
 
+template <bool AGAIN>
 __device__ __forceinline__ float block_sum(float v, float *park, int waves)
 {
     v = wave_sum_dpp(v);
-    __syncthreads();   // the numbers of the row before have been read
+    if constexpr (AGAIN)
+        __syncthreads();   // the numbers of the row before have been read
     if ((threadIdx.x & 63) == 0)
         park[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -26,19 +28,19 @@ __device__ __forceinline__ float block_sum(float v, float *park, int waves)
 }
 
 /*
- * 1 / sqrt(sum * share + eps), rounded once: the fp32 value of four roundings takes one Newton step in 64 bits, since a row's every
- * element carries its error, and with it the codes that lie next to a rounding's edge.  (A step with t = m r, r += r (1 - t r) / 2,
- * squares the error.)  Nothing for 0, NaN for what fp32 does not hold.
+ * 1 / sqrt(sum * share + eps), rounded once: a row's every element carries its error, and with it the codes that lie next to a
+ * rounding's edge (four roundings in fp32: error of the codes against 64 bits 5.1e-5 at 16384 x 2048, so 6.9e-6).  In 64 bits, from
+ * the hardware's reciprocal root, good to some 24 bits, by one Newton step, which squares the error.  Nothing for 0, NaN for a sum
+ * that fp32 does not hold.
  */
 __device__ __forceinline__ float reciprocal_root(float sum, double share, float eps)
 {
     const double m = __fma_rn((double)sum, share, (double)eps);
-    const float mean = (float)m;
-    if (mean == 0.0f)
+    if (m == 0.0)
         return 0.0f;
-    if (!(mean < INFINITY))
+    if (!(sum < INFINITY))
         return NAN;
-    const double r = 1.0f / sqrtf(mean);
+    const double r = __builtin_amdgcn_rsq(m);
     return (float)__fma_rn(0.5 * r, __fma_rn(-m * r, r, 1.0), r);
 }
 
@@ -94,7 +96,7 @@ __global__ __launch_bounds__(kRowThreads) void rms_norm_kernel(const T *__restri
         for (int e = 0; e < 8; ++e)
             sum = __fmaf_rn(v[i][e], v[i][e], sum);
     }
-    const float rstd = reciprocal_root(block_sum(sum, park, threads / kWave), 1.0 / cols, eps);
+    const float rstd = reciprocal_root(block_sum<false>(sum, park, threads / kWave), 1.0 / cols, eps);
     if (rstd_out && threadIdx.x == 0)
         rstd_out[row] = rstd;
 #pragma unroll
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(backward_threads(GROUP)) void rms_norm_backward_ker
                 }
             }
         }
-        const float mean = (GROUP == 1 ? wave_sum_dpp(sum) : block_sum(sum, park, GROUP)) / (float)cols;
+        const float mean = (GROUP == 1 ? wave_sum_dpp(sum) : block_sum<true>(sum, park, GROUP)) / (float)cols;
         if (mine) {
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
