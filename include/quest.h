@@ -387,8 +387,8 @@ int64_t quest_grad_gemm_mx_workspace_bytes(int32_t which, int64_t M, int64_t N, 
  *   y_out      out [rows, cols] of dtype, or NULL;  rstd   out [rows] fp32, or NULL (what the backward pass reads)
  *   codes, scales, mask   out, or codes = scales = mask = NULL (then had_block and format are not looked at, and y_out is needed)
  *   had_block  power of two that divides cols, at most QUEST_MAX_NORM_HAD_BLOCK
- * A row of zeros, or one whose sum of squares is zero in fp32, gives rstd = 0 and y = 0 with eps = 0.  A row with an infinity or a NaN, or whose sum of squares exceeds the
- * fp32 range, gives NaN throughout (rstd, y, scale bytes 255).
+ * A row of zeros, or one whose sum of squares is zero in fp32, gives rstd = 0 and y = 0 with eps = 0.  A row with an infinity or
+ * a NaN, or whose sum of squares exceeds the fp32 range, gives NaN throughout (rstd, y, scale bytes 255).
  * Everything but scales (any alignment) and rstd (4 bytes) 16-byte aligned, row strides in bytes too.
  */
 quest_status quest_rms_norm_mx(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual, quest_dtype dtype,
