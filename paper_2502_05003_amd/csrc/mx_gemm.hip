@@ -273,7 +273,9 @@ hipError_t launch_few_groups(const MxGemmArgs &a, hipStream_t stream)
 template <int FORMAT>
 hipError_t launch_format(const MxGemmArgs &a, hipStream_t stream)
 {
-    const quest_plan p = plan_mx_gemm(a.M, a.N, a.K);
+    quest_plan p = plan_mx_gemm(a.M, a.N, a.K);
+    if (p.kernel == QUEST_PLAN_TILES && a.y && a.ld_y >= (1 << 24))   // a tile's 32 rows of y are one buffer of less than 2 GiB
+        p = {QUEST_PLAN_FEW, 64, 64, 0};
     if (p.kernel == QUEST_PLAN_TILES)
         return FORMAT == QUEST_MX_E4M3 ? launch_mx_tiles_e4m3(a, p.block_rows, stream) : launch_mx_tiles_e2m1(a, p.block_rows, stream);
     if (p.block_cols == 16)

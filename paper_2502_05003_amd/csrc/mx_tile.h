@@ -15,11 +15,12 @@
 // are issued behind their stage's transfers and counted, so that nothing waits for them before the end of the stage that follows
 // (16384 x 5632 x 2048 132 -> 124 us, 16384 x 4096 x 1024 67 -> 62).
 //
-// What bounds it: with large contractions the chip's power (4096 x 4096 x 16640 in E2M1 139 us or 4.0 PFLOP/s; with operands of
-// zeros 103, and the matrix instructions alone, from registers, sustain 6.5), with short ones the tiles' ends on top (16384 x 5632
-// x 2048 114 us, 40 of them the output at the rate of a large copy).  Tried and dropped: each stage in two groups of transfers
-// with a whole stage's time each, for a second barrier per stage (4096 x 4096 x 4096 41 -> 45 us); lines asked for two stages
-// ahead (120 -> 140); all transfers in phase 1 or spread over all phases (the same within 2 %).
+// What bounds it: with large contractions the chip's power (4096 x 4096 x 16640 in E2M1 139 to 148 us, 3.8 to 4.0 PFLOP/s; with
+// operands of zeros 103, where the wave's instructions are the bound, one in 8 cycles; the matrix instructions alone, from
+// registers, sustain 6.5), with short ones the tiles' ends on top (16384 x 5632 x 2048 119 us, 36 of them the output at the rate of
+// a large copy; matrix pipes 0.33 busy).  Tried and dropped: each stage in two groups of transfers with a whole stage's time each, for a
+// second barrier per stage (4096 x 4096 x 4096 41 -> 45 us); lines asked for two stages ahead (120 -> 140); all transfers in
+// phase 1 or spread over all phases (the same within 2 %).
 #pragma once
 
 #include <algorithm>
@@ -32,6 +33,7 @@ namespace {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
 constexpr int kUnit = 128;                 // elements of a matrix instruction
 constexpr int kF4 = 4, kF8 = 0;            // its codes for E2M1 and E4M3
@@ -84,48 +86,15 @@ enum {
     kStageLast = 4        // the last of its tile
 };
 
-// One piece of 32 rows by 64 columns, parked with 16-byte chunk c of row r at c ^ (r & 7), where whole 16-byte stores do not do
-__device__ __forceinline__ void store_ragged_piece(const uint8_t *park, uint16_t *__restrict__ y, int64_t ld_y, int row0, int col0,
-                                                int M, int N, int lane)
-{
-    uint16_t *const base = y + (int64_t)row0 * ld_y + col0;
-    auto parked = [&](int row, int col) { return park + row * 128 + (((col >> 3) ^ (row & 7)) << 4) + (col & 7) * 2; };
-    if ((ld_y & 7) == 0 && (reinterpret_cast<uintptr_t>(y) & 15) == 0) {
-        const int c = 8 * (lane & 7), left = N - col0 - c;
-        for (int row = lane >> 3; row < 32 && row0 + row < M; row += 8) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(parked(row, c));
-            uint16_t *dst = base + (int64_t)row * ld_y + c;
-            if (left >= 8) {
-                *reinterpret_cast<uint4 *>(dst) = v;
-            } else {
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int e = 0; e < 7; ++e)
-                    if (e < left)
-                        dst[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
-            }
-        }
-        return;
-    }
-    if ((ld_y & 1) == 0 && (reinterpret_cast<uintptr_t>(y) & 3) == 0) {   // consecutive columns, two to a lane
-        const int c = 2 * (lane & 31);
-        for (int row = lane >> 5; row < 32 && row0 + row < M; row += 2) {
-            const uint32_t v = *reinterpret_cast<const uint32_t *>(parked(row, c));
-            uint16_t *dst = base + (int64_t)row * ld_y + c;
-            if (col0 + c + 1 < N)
-                *reinterpret_cast<uint32_t *>(dst) = v;
-            else if (col0 + c < N)
-                *dst = (uint16_t)v;
-        }
-        return;
-    }
-    for (int row = 0; row < 32 && row0 + row < M; ++row)
-        if (col0 + lane < N)
-            base[(int64_t)row * ld_y + lane] = *reinterpret_cast<const uint16_t *>(parked(row, lane));
-}
+// what a kernel stores
+enum {
+    kWholePieces = 0,     // y in 16-byte pieces: rows and columns that fit them
+    kAnyRows = 1,         // y of any width, pitch and start
+    kRawSums = 2          // the fp32 sums, and y as above, if it is wanted
+};
 
-// TWO: tiles of two stages (else more); GENERAL: rows of y that 16-byte stores do not fit, or raw accumulators
-template <int FORMAT, int WI, int WJ, bool TWO, bool GENERAL>
+// TWO: tiles of two stages (else more)
+template <int FORMAT, int WI, int WJ, bool TWO, int OUT>
 __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
     const uint8_t *__restrict__ a_codes, const uint8_t *__restrict__ a_scales, const uint8_t *__restrict__ b_codes,
     const uint8_t *__restrict__ b_scales, int M, int N, int K, int tiles_m, int tiles_n, uint16_t *__restrict__ y, int64_t ld_y,
@@ -286,17 +255,22 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
     constexpr int kOutParts = (WJ / 2) * 6;
     auto store_part = [&](auto block, auto part) __attribute__((always_inline)) {
         constexpr int i = decltype(block)::value, piece = decltype(part)::value / 6, n = decltype(part)::value % 6;
-        if constexpr (GENERAL && n == 0 && piece == 0) {
-            if (acc_out)
-                static_for<2 * NJ>([&](auto tc) {
-                    constexpr int u = decltype(tc)::value / NJ, j = decltype(tc)::value % NJ;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int m = out_m + 32 * i + 16 * u + l16, col = out_n + 16 * j + 4 * quarter + e;
-                        if (m < M && col < N)
-                            acc_out[(int64_t)m * N + col] = acc[2 * i + u][j][e];
-                    }
-                });
+        // rows and columns that do not exist lie outside of the buffers
+        const int rows = min(max(M - out_m - 32 * i, 0), 32);
+        constexpr uint32_t kNowhere = 0x80000000u;
+        if constexpr (OUT == kRawSums && n == 0 && piece == 0) {
+            const auto buffer = __builtin_amdgcn_make_buffer_rsrc(acc_out + (int64_t)(out_m + 32 * i) * N + out_n, 0, rows * N * 4,
+                                                                  0x00027000);
+            static_for<2 * NJ>([&](auto tc) {
+                constexpr int u = decltype(tc)::value / NJ, j = decltype(tc)::value % NJ;
+                const int left = N - out_n - 16 * j - 4 * quarter, tail = left > 0 && left < 4 ? left : 0;
+                const uint32_t at = ((uint32_t)(16 * u + l16) * (uint32_t)N + 16u * j + 4u * quarter) * 4u;
+                const auto sum = __builtin_bit_cast(quest_v4u, acc[2 * i + u][j]);
+                __builtin_amdgcn_raw_buffer_store_b128(sum, buffer, (int)(left >= 4 ? at : kNowhere), 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b64(v2u{sum[0], sum[1]}, buffer, (int)(tail & 2 ? at : kNowhere), 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b32(tail & 2 ? sum[2] : sum[0], buffer,
+                                                      (int)(tail & 1 ? at + 4u * (tail & 2) : kNowhere), 0, 0);
+            });
         }
         if constexpr (n < 4) {             // columns 16 n .. + 16 of the piece
             static_for<2>([&](auto uc) {
@@ -305,9 +279,6 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
                 *reinterpret_cast<uint2 *>(park + (16 * u + l16) * 128 + (((2 * n + (quarter >> 1)) ^ (l16 & 7)) << 4) + 8 * (quarter & 1)) =
                     make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
             });
-        } else if constexpr (GENERAL) {
-            if (n == 5 && y && out_m + 32 * i < M && out_n + 64 * piece < N)
-                store_ragged_piece(park, y, ld_y, out_m + 32 * i, out_n + 64 * piece, M, N, lane);
         } else if constexpr (n == 4) {
 #pragma unroll
             for (int pass = 0; pass < 4; ++pass) {
@@ -315,14 +286,27 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
                 out_reg[pass] = *reinterpret_cast<const quest_v4u *>(park + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
             }
         } else {
-            // rows and columns that do not exist lie outside of the buffer (columns come in eights)
-            const int rows = min(max(M - out_m - 32 * i, 0), 32);
-            const auto buffer = __builtin_amdgcn_make_buffer_rsrc(y + (int64_t)(out_m + 32 * i) * ld_y + out_n + 64 * piece, 0,
-                                                                  rows * (int)ld_y * 2, 0x00027000);
-            const uint32_t at = out_n + 64 * piece + 8 * (lane & 7) < N ? y_lane : 0x80000000u;
+            // (any two-byte boundary will do for these stores; the buffer itself begins at a dword)
+            const uint64_t place = reinterpret_cast<uint64_t>(y + (int64_t)(out_m + 32 * i) * ld_y + out_n + 64 * piece);
+            const uint32_t odd = OUT == kWholePieces ? 0u : (uint32_t)place & 2u;
+            const auto buffer = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(place - odd), 0,
+                                                                  OUT == kWholePieces || y ? rows * (int)ld_y * 2 + (int)odd : 0, 0x00027000);
+            const int left = N - out_n - 64 * piece - 8 * (lane & 7), tail = left > 0 && left < 8 ? left : 0;
+            const uint32_t at = y_lane + odd;
 #pragma unroll
-            for (int pass = 0; pass < 4; ++pass)
-                __builtin_amdgcn_raw_buffer_store_b128(out_reg[pass], buffer, (int)(at + (uint32_t)(8 * pass) * (uint32_t)ld_y * 2u), 0, 0);
+            for (int pass = 0; pass < 4; ++pass) {
+                const uint32_t down = (uint32_t)(8 * pass) * (uint32_t)ld_y * 2u;
+                const quest_v4u &v = out_reg[pass];
+                __builtin_amdgcn_raw_buffer_store_b128(v, buffer, (int)((left >= 8 || (OUT == kWholePieces && left > 0) ? at : kNowhere) + down), 0, 0);
+                if constexpr (OUT != kWholePieces) {   // four, two and one of a row's last columns
+                    __builtin_amdgcn_raw_buffer_store_b64(v2u{v[0], v[1]}, buffer, (int)((tail & 4 ? at : kNowhere) + down), 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b32(tail & 4 ? v[2] : v[0], buffer,
+                                                          (int)((tail & 2 ? at + 2u * (tail & 4) : kNowhere) + down), 0, 0);
+                    const uint32_t last = tail & 4 ? (tail & 2 ? v[3] : v[2]) : tail & 2 ? v[1] : v[0];
+                    __builtin_amdgcn_raw_buffer_store_b16((short)last, buffer,
+                                                          (int)((tail & 1 ? at + 2u * (tail & 6) : kNowhere) + down), 0, 0);
+                }
+            }
         }
     };
 
@@ -371,7 +355,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
         // transfers spread over phases 1 and 2, in E2M1, which has more of them, over 3 (4096 x 4096 x 16640: 143 -> 139 us);
         // where a tile before ends, all of them ahead of its stores
         constexpr int kDmaSlots = boundary ? 5 * kFragB / kOutParts + 1 : (kE4M3 || WI < 4 ? 2 : 3) * kFragB;
-        constexpr int kStoresBehind = [] {   // the last of them
+        constexpr int kStoresBehind = [] {   // the last of them, at least
             int count = 0;
             for (int number = boundary ? 0 : 2; number < (boundary ? 2 : last ? WI : 0); ++number)
                 for (int piece = 0; piece < WJ / 2; ++piece)
@@ -424,7 +408,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
         // The reads of block WI - 1 are back, the next stage has landed.  Stores, which were issued behind its transfers, may be on
         // their way until the stage behind it has landed.
         __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
-        wait_vmcnt<GENERAL ? 0 : kStoresBehind>();
+        wait_vmcnt<kStoresBehind>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");        // no read of the new stage ahead of it
         cur ^= 1;
@@ -480,13 +464,15 @@ hipError_t launch_tiles(const MxGemmArgs &a, hipStream_t stream)
     typedef MxTile<FORMAT, WI, WJ> T;
     const int tiles_m = (int)((a.M + T::kRows - 1) / T::kRows), tiles_n = (int)((a.N + T::kCols - 1) / T::kCols);
     const int per_xcd = (int)(((int64_t)tiles_m * tiles_n + 7) / 8), peers = std::min(per_xcd, device_compute_units() / 8);
-    // (a tile's rows as one buffer: byte offsets below 2^31)
-    const bool pieces_fit = a.y && !a.acc_out && (a.ld_y & 7) == 0 && (a.N & 7) == 0 && a.ld_y < (1 << 24) &&
-                            (reinterpret_cast<uintptr_t>(a.y) & 15) == 0;
-    auto kernel = pieces_fit ? mx_tile_kernel<FORMAT, WI, WJ, false, false> : mx_tile_kernel<FORMAT, WI, WJ, false, true>;
+    const bool whole = (a.ld_y & 7) == 0 && (a.N & 7) == 0 && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0;
+    auto kernel = a.acc_out ? mx_tile_kernel<FORMAT, WI, WJ, false, kRawSums>
+                  : whole   ? mx_tile_kernel<FORMAT, WI, WJ, false, kWholePieces>
+                            : mx_tile_kernel<FORMAT, WI, WJ, false, kAnyRows>;
     if constexpr (!T::kE4M3) {   // (in E4M3 the shortest contraction has three)
         if (a.K <= 2 * T::kStageK)
-            kernel = pieces_fit ? mx_tile_kernel<FORMAT, WI, WJ, true, false> : mx_tile_kernel<FORMAT, WI, WJ, true, true>;
+            kernel = a.acc_out ? mx_tile_kernel<FORMAT, WI, WJ, true, kRawSums>
+                     : whole   ? mx_tile_kernel<FORMAT, WI, WJ, true, kWholePieces>
+                               : mx_tile_kernel<FORMAT, WI, WJ, true, kAnyRows>;
     }
     hipLaunchKernelGGL(kernel, dim3((unsigned)(8 * peers)), dim3(kTileThreads), T::kLds, stream, a.a_codes, a.a_scales, a.b_codes,
                        a.b_scales, (int)a.M, (int)a.N, (int)a.K, tiles_m, tiles_n, static_cast<uint16_t *>(a.y), a.ld_y, a.acc_out);
@@ -502,16 +488,19 @@ hipError_t prepare_tiles()
         if (err == hipSuccess)
             err = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), kLds);
     };
-    allow(mx_tile_kernel<FORMAT, WI, WJ, false, false>);
-    allow(mx_tile_kernel<FORMAT, WI, WJ, false, true>);
+    allow(mx_tile_kernel<FORMAT, WI, WJ, false, kWholePieces>);
+    allow(mx_tile_kernel<FORMAT, WI, WJ, false, kAnyRows>);
+    allow(mx_tile_kernel<FORMAT, WI, WJ, false, kRawSums>);
     if constexpr (!MxTile<FORMAT, WI, WJ>::kE4M3) {
-        allow(mx_tile_kernel<FORMAT, WI, WJ, true, false>);
-        allow(mx_tile_kernel<FORMAT, WI, WJ, true, true>);
+        allow(mx_tile_kernel<FORMAT, WI, WJ, true, kWholePieces>);
+        allow(mx_tile_kernel<FORMAT, WI, WJ, true, kAnyRows>);
+        allow(mx_tile_kernel<FORMAT, WI, WJ, true, kRawSums>);
     }
     return err;
 }
 
-// a.M, a.N of any size, a.K >= 384, which are two stages or more; tiles of `block` x `block`: 256 or 128
+// a.M, a.N of any size, a.K >= 384, which are two stages or more, rows of y less than 2^24 elements
+// apart; tiles of `block` x `block`: 256 or 128
 template <int FORMAT>
 hipError_t launch_mx_tiles(const MxGemmArgs &a, int block, hipStream_t stream)
 {

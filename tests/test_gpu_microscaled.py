@@ -275,6 +275,22 @@ def test_large_product_of_columns_that_16_bytes_do_not_divide(N):
             assert bool((flat[start + M * (N + pitch):] == -7.0).all())
 
 
+def test_product_into_rows_far_apart():
+    """Offsets into y beyond 2^32 bytes, and a pitch that the tiles' buffers do not take."""
+    M, N, K, pitch = 129, 5504, 384, (1 << 24) + 8
+    (ac, as_), (bc, bs) = random_operand(M, K, E2M1, 1), random_operand(N, K, E2M1, 2)
+    dev = on_device(ac, as_) + on_device(bc, bs)
+    ref = torch.empty(M, N, dtype=BF16, device=DEV)
+    q.quest_lowbit_gemm_mx(dev[0], dev[1], E2M1, dev[2], dev[3], K, y=ref)
+    y = torch.empty(M * pitch, dtype=BF16, device=DEV).view(M, pitch)[:, :N]
+    y.fill_(-7.0)
+    q.quest_lowbit_gemm_mx(dev[0], dev[1], E2M1, dev[2], dev[3], K, y=y)
+    a, b = mx.values(ac, as_, E2M1), mx.values(bc, bs, E2M1)
+    exact, bound = (torch.from_numpy(t).to(DEV) for t in (a @ b.T, product_bound(a, b, E2M1)))
+    for got in (ref, y):      # the two kernels sum in different orders; 2^-8: one rounding to bf16, of the sum with its error
+        assert bool(((got.double() - exact).abs() <= 2.0 ** -8 * exact.abs() + 1.01 * bound).all())
+
+
 @pytest.mark.parametrize("M,N,K", [(5, 70, 256), (300, 322, 256)])
 @pytest.mark.parametrize("pitch", [0, 1, 2, 6, 8])
 def test_product_into_wider_rows(M, N, K, pitch):
