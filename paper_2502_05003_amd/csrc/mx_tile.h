@@ -26,6 +26,7 @@
 #include <algorithm>
 
 #include "mx_formats.h"
+#include "mx_stages.h"
 #include "quest_internal.h"
 
 namespace quest {
@@ -35,18 +36,16 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
-constexpr int kUnit = 128;                 // elements of a matrix instruction
 constexpr int kF4 = 4, kF8 = 0;            // its codes for E2M1 and E4M3
 constexpr int kTileThreads = 256;
 constexpr int kParkBytes = 32 * 128;       // 32 rows by 64 columns in bf16
-constexpr int kScaleChunk = 512;           // elements whose scales one transfer of 16 bytes per row brings
 
 template <int FORMAT, int WI, int WJ>
 struct MxTile {
     static constexpr bool kE4M3 = FORMAT == QUEST_MX_E4M3;
     static constexpr int kRows = 64 * WI, kCols = 64 * WJ;
     static constexpr int kSteps = kE4M3 ? 1 : 2;                 // matrix instructions along a stage
-    static constexpr int kStageK = kUnit * kSteps;
+    typedef MxStages<kSteps> Stages;
     static constexpr int kRowA = 128, kRowB = 64 * kSteps;       // bytes of a row in a stage
     static constexpr int kBytesA = kRows * kRowA, kStage = kBytesA + kCols * kRowB;
     static constexpr int kScales = (kRows + kCols) * 16;
@@ -121,9 +120,8 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
     const uint32_t smem_addr = lds_address(smem);
     const int64_t row_a = kE4M3 ? K : K / 2, row_b = K / 2;
     const int row_scales = K / 32;                       // bytes
-    const int stages = (K + T::kStageK - 1) / T::kStageK;
-    const bool half_stage = K % T::kStageK != 0;         // E2M1: the last stage of a tile holds 128 elements
-    const int words = K / 128;                           // scale dwords of a row
+    const int stages = T::Stages::count(K);
+    const bool half_stage = T::Stages::ends_in_half(K);  // E2M1: the last stage of a tile holds 128 elements
 
     // ---- transfers, one stage ahead of the multiplication.  One moves 1 KiB: lane l lands at 16 l, so it fetches the chunk that
     // belongs there (see the reads below).  The rows of a tile are a buffer that ends with the operand: transfers of rows beyond
@@ -176,9 +174,6 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
     };
     const uint32_t scale_at = (uint32_t)lane * (uint32_t)row_scales;
     const uint32_t scale_addr = smem_addr + 2 * T::kStage;
-    // first scale dword of the 16 bytes that hold a stage's (the last ones of a row end where the row ends; a row of three is
-    // followed by something that no stage uses)
-    auto chunk_start = [&](int at) { return max(min(at * T::kStageK / kScaleChunk * 4, words - 4), 0); };
     auto transfer_scales = [&](int buffer, int at) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < (WI + WJ + 3) / 4; ++h) {
@@ -187,7 +182,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
             if (piece >= WI + WJ)
                 continue;
             lds_buffer16_at<0>(buffer_of(left ? fetch_as : fetch_bs, (left ? fetch_rows_a : fetch_rows_b) * (uint32_t)row_scales),
-                               scale_at + (uint32_t)(64 * (left ? piece : piece - WI) * row_scales + 4 * chunk_start(at)),
+                               scale_at + (uint32_t)(64 * (left ? piece : piece - WI) * row_scales + 4 * T::Stages::chunk(at)),
                                scale_addr + buffer * T::kScales + piece * 1024);
         }
     };
@@ -208,14 +203,13 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
         constexpr int f = decltype(frag)::value, t = f / NJ, j = f % NJ;
         bf[f] = *reinterpret_cast<const uint4 *>(stage + (b_lane ^ (t << 6)) + 16 * j * T::kRowB);
     };
-    // A row's scales of a stage begin at dword `word` of its 16 bytes; the lane's byte is that of its quarter.  (E2M1: a pair that
-    // would begin at an odd dword belongs to a half stage, which has the first one only.)
+    // A row's scales of a stage begin at dword `word` of its chunk (E2M1: a pair); the lane's byte is that of its quarter
     const uint32_t pick_pair = 0x0c0c0000u | (uint32_t)(4 + quarter) << 8 | (uint32_t)quarter;
-    const uint32_t pick_first = 0x0c0c0c00u | (uint32_t)quarter, pick_second = 0x0c0c0c04u + (uint32_t)quarter;
+    const uint32_t pick_first = 0x0c0c0c00u | (uint32_t)quarter;
     auto read_scale = [&](int buffer, int word, int row) __attribute__((always_inline)) {
         const uint8_t *at = smem + 2 * T::kStage + buffer * T::kScales + row * 16;
         if constexpr (T::kSteps == 2)
-            return *reinterpret_cast<const uint2 *>(at + (word & 2) * 4);
+            return *reinterpret_cast<const uint2 *>(at + word * 4);
         else
             return *reinterpret_cast<const uint32_t *>(at + word * 4);
     };
@@ -324,20 +318,20 @@ __global__ __launch_bounds__(kTileThreads, 1) void mx_tile_kernel(
         }
         const int fetched = last ? 0 : at + 1;
         const bool fetched_half = !kE4M3 && half_stage && fetched == stages - 1;
-        const bool new_scales = fetched * T::kStageK % kScaleChunk == 0;
+        const bool new_scales = T::Stages::opens_chunk(fetched);
         if (new_scales)
             transfer_scales(scale_buffer ^ 1, fetched);
         // This stage's scales: read during phase 1, whose products need those of the stage before
         uint32_t sb_new[NJ];
         const uint32_t sa_before[2] = {sa[WI - 1][0], sa[WI - 1][1]};
-        const int word = at * T::kSteps - chunk_start(at);
+        const int word = T::Stages::word(at);
         constexpr int kRowScales = 2 * WI + NJ, kPerSlot = (kRowScales + kFragB - 1) / kFragB, kBehind = 4 / kPerSlot;
         decltype(read_scale(0, 0, 0)) raw[kRowScales];
         // The second half of a half stage holds the first one's codes again: with scales of 2^-127 on both sides their products
         // (below 2^-240) leave the fp32 sums as they are.
         uint32_t pick = T::kSteps == 2 ? pick_pair : 8u * quarter;
         if constexpr (last && !kE4M3)
-            pick = !half_stage ? pick : (word & 1) ? pick_second : pick_first;
+            pick = half_stage ? pick_first : pick;
         auto scale_slot = [&](auto slot) __attribute__((always_inline)) {
             static_for<kPerSlot>([&](auto more) {
                 constexpr int now = decltype(slot)::value * kPerSlot + decltype(more)::value, then = now - kBehind * kPerSlot;
@@ -469,7 +463,7 @@ hipError_t launch_tiles(const MxGemmArgs &a, hipStream_t stream)
                   : whole   ? mx_tile_kernel<FORMAT, WI, WJ, false, kWholePieces>
                             : mx_tile_kernel<FORMAT, WI, WJ, false, kAnyRows>;
     if constexpr (!T::kE4M3) {   // (in E4M3 the shortest contraction has three)
-        if (a.K <= 2 * T::kStageK)
+        if (T::Stages::count((int)a.K) == 2)
             kernel = a.acc_out ? mx_tile_kernel<FORMAT, WI, WJ, true, kRawSums>
                      : whole   ? mx_tile_kernel<FORMAT, WI, WJ, true, kWholePieces>
                                : mx_tile_kernel<FORMAT, WI, WJ, true, kAnyRows>;

@@ -257,6 +257,18 @@ def test_large_product(M, N, K, fmt):
     assert torch.equal(odd[:, :N], y) and bool((odd[:, N:] == -7.0).all())
 
 
+# a tile's scales come in chunks of 512 elements of a row: contractions of several chunks with each remainder, for both blocks, in the
+# workgroups' first tiles and in those behind them
+CHUNKED_PRODUCTS = [(2100, 2200, 896), (2303, 2056, 1408), (1290, 2060, 1920), (4097, 1288, 1024), (2100, 2200, 1280),
+                    (6000, 4104, 896), (2600, 4104, 1408), (1800, 5128, 1920), (2600, 4104, 1024), (2600, 4104, 1280), (6000, 4104, 1664)]
+
+
+@pytest.mark.parametrize("M,N,K", CHUNKED_PRODUCTS)
+@pytest.mark.parametrize("fmt", [E2M1, E4M3])
+def test_large_product_of_several_chunks_of_scales(M, N, K, fmt):
+    test_large_product(M, N, K, fmt)
+
+
 @pytest.mark.parametrize("N", [2049, 2050, 2060])
 def test_large_product_of_columns_that_16_bytes_do_not_divide(N):
     M, K = 2080, 640

@@ -433,3 +433,61 @@ def test_products_reach_every_kernel():
         assert {K % 256 for M, N, K in of} == {0, 128} and {384, 512} <= {K for M, N, K in of}
     assert mx_plan(1, 1 << 22, 65536)[0] == "few" and mx_plan(1 << 22, 1 << 22, 256) == ("few", 64, 64)
     assert mx_plan(1 << 22, 1 << 22, 384) == ("tiles", 256, 256)
+
+
+def test_products_of_several_chunks_of_scales_reach_both_tiles():
+    """Scales are staged 512 elements at a time: each remainder by that, with more than one chunk, with both blocks, in the
+    workgroups' first tiles and in further ones."""
+    import test_gpu_microscaled as gpu
+    for block in (128, 256):
+        of = [s for s in gpu.LARGE_PRODUCTS + gpu.CHUNKED_PRODUCTS if mx_plan(*s) == ("tiles", block, block) and s[2] > 512]
+        assert {K % 512 for _, _, K in of} == {0, 128, 256, 384}
+        for tiles_of_a_workgroup in (False, True):
+            assert any(K % 512 == 384 and (-(-M // block) * -(-N // block) > 256) == tiles_of_a_workgroup for M, N, K in of), block
+
+
+# what the kernel does with the header: transfers into two buffers of a chunk in turn, reads of a dword or of an aligned pair
+STAGES = r"""
+#include <stdio.h>
+#include "mx_stages.h"
+
+template <int STEPS>
+int check()
+{
+    typedef quest::MxStages<STEPS> S;
+    int bad = 0;
+    for (int K = 384; K <= 65536; K += 128) {
+        const int units = K / 128, stages = S::count(K);
+        bad += stages < 2 || (stages - 1) * S::kStageK >= K || stages * S::kStageK < K || S::ends_in_half(K) != (units % STEPS != 0);
+        int held = -1;
+        for (int at = 0; at < stages; ++at) {
+            if (S::opens_chunk(at))
+                held = S::chunk(at);
+            bad += held != S::chunk(at) || S::chunk(at) >= units;          // (its first dword is one of the row's)
+            bad += S::word(at) % STEPS != 0 || S::word(at) + STEPS > S::kChunk;
+            const int real = at == stages - 1 && S::ends_in_half(K) ? 1 : STEPS;
+            for (int t = 0; t < real; ++t)
+                bad += held + S::word(at) + t != at * STEPS + t || at * STEPS + t >= units;
+            if (at == stages - 1)
+                bad += at * STEPS + real != units;
+        }
+        bad += S::chunk(0) != 0 || !S::opens_chunk(0);                     // a tile's first stage
+    }
+    return bad;
+}
+
+int main()
+{
+    printf("%d %d\n", check<1>(), check<2>());
+    return 0;
+}
+"""
+
+
+def test_stages_find_their_scales(tmp_path):
+    """All contractions that tiles take: each stage reads its own scale dwords, out of the chunk that the transfers left last."""
+    source, program = tmp_path / "check.hip", str(tmp_path / "check")
+    source.write_text(STAGES)
+    subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), "--offload-arch=gfx950", "-O1", "-std=c++17", "-I", build.CSRC,
+                    str(source), "-o", program], check=True, capture_output=True)
+    assert subprocess.run([program], check=True, capture_output=True, text=True).stdout.split() == ["0", "0"]
