@@ -141,7 +141,7 @@ def _native_calls(lib):
             return tuple(kind(*(ctypes.cast(getattr(lib, name), _p).value for name in names))
                          for kind, names in ((quest_python.Calls, _NATIVE), (quest_python.MxCalls, _MX_NATIVE)))
         why = f"it was built for {built_for}, this is {torch_build()}"
-    except ImportError as error:
+    except (ImportError, AttributeError, TypeError) as error:   # the latter two: it was built from other sources
         why = str(error)
     warnings.warn(f"the native module quest_python is not used, calls take 3 us more ({why}); to build it: "
                   "`python -c 'import __graft_entry__ as g; g.build()'`", RuntimeWarning, stacklevel=3)

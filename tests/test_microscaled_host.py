@@ -5,6 +5,7 @@ import inspect
 import os
 import re
 import subprocess
+import sys
 import types
 
 import numpy as np
@@ -330,6 +331,28 @@ def test_what_is_refused_reaches_no_entry_point(record, monkeypatch):
         with pytest.raises(RuntimeError, match="no device"):
             getattr(q, name)(*args, **kwargs)
     assert not record.seen
+
+
+def fewer_addresses(*addresses):
+    raise TypeError("one address for each entry point")
+
+
+@pytest.mark.parametrize("kinds", [dict(), dict(MxCalls=fewer_addresses)])
+def test_with_a_native_module_of_other_entry_points_calls_take_the_general_way(kinds, record, monkeypatch):
+    """One built for this torch, but from other sources: without these calls, or with another number of them."""
+    import paper_2502_05003_amd as package
+    from paper_2502_05003_amd import quest_python
+    module = types.SimpleNamespace(TORCH_BUILD=q.torch_build(), Calls=quest_python.Calls, **kinds)
+    monkeypatch.setattr(package, "quest_python", module)
+    monkeypatch.setitem(sys.modules, package.__name__ + ".quest_python", module)
+    monkeypatch.setattr(q, "_lib", None)
+    with pytest.warns(RuntimeWarning, match="g.build()"):
+        assert q.quest_container_bits(4) == 4
+    record.library.mx_calls = q.load().mx_calls
+    monkeypatch.setattr(q, "_lib", record.library)
+    for name, args, kwargs in mx_calls(torch.bfloat16):
+        getattr(q, name)(*args, **kwargs)
+        assert record.seen[-1][0] == name
 
 
 SIGNATURES = {
