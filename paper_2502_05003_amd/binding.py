@@ -438,7 +438,8 @@ def _code_bytes(fmt: int, cols: int) -> int:
 
 def _operand(codes: torch.Tensor | None, scales: torch.Tensor | None, mask: torch.Tensor | None, fmt: int, rows: int, cols: int,
              name: str = "") -> None:
-    _packed(codes, name + "codes", torch.uint8, (rows, _code_bytes(fmt, cols)))
+    if codes is not None:
+        _packed(codes, name + "codes", torch.uint8, (rows, _code_bytes(fmt, cols)))
     _packed(scales, name + "scales", torch.uint8, (rows, cols // QUEST_MX_GROUP))
     _packed(mask, name + "mask", torch.uint8, (rows, cols // 8))
 
@@ -518,7 +519,8 @@ def quest_rms_norm_mx(x: torch.Tensor, weight: torch.Tensor, eps: float, had_blo
                       codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, mask: torch.Tensor | None = None,
                       residual: torch.Tensor | None = None, h_out: torch.Tensor | None = None, y_out: torch.Tensor | None = None,
                       rstd: torch.Tensor | None = None) -> None:
-    """h_out = x + residual; y_out = h * rstd * weight; codes, scales, mask: y as quest_hadamard_quantize_mx quantizes it."""
+    """h_out = x + residual; y_out = h * rstd * weight; codes, scales, mask: y as quest_hadamard_quantize_mx quantizes it (without
+    them had_block and fmt are not looked at)."""
     status = (_lib or load()).mx_calls.rms_norm_mx(x, weight, eps, had_block, fmt, codes, scales, mask, residual, h_out,
                                                    y_out, rstd, _stream, _current_device)
     if status is None:

@@ -521,8 +521,7 @@ PyObject *mx_rms_norm(PyObject *self, PyObject *const *args, Py_ssize_t count)
     MxReader r(args, count, 14);
     const at::Tensor *x = r.matrix(), *weight = r.tensor();
     const float eps = r.f32();
-    const int32_t block = r.i32();
-    const quest_mx_format format = r.format();
+    const int32_t block = r.i32(), asked = r.i32();   // (both are looked at where there are codes)
     const at::Tensor *codes = r.tensor_or_none(), *scales = r.tensor_or_none(), *mask = r.tensor_or_none();
     const at::Tensor *residual = r.tensor_or_none(), *h = r.tensor_or_none(), *y = r.tensor_or_none(), *rstd = r.tensor_or_none();
     PyObject *ask_stream = r.object(), *ask_device = r.object();
@@ -530,6 +529,8 @@ PyObject *mx_rms_norm(PyObject *self, PyObject *const *args, Py_ssize_t count)
     const int64_t rows = r.size(x, 0), cols = r.size(x, 1), ld_x = r.rows_of(x, rows, cols);
     r.require(r.plain && (!residual || residual->scalar_type() == x->scalar_type()));
     const int64_t ld_residual = residual ? r.rows_of(residual, rows, cols) : 0;
+    r.require(!codes || asked == QUEST_MX_E2M1 || asked == QUEST_MX_E4M3);
+    const quest_mx_format format = (quest_mx_format)asked;
     r.operand(codes, scales, mask, format, rows, cols);
     if (r.plain) {
         r.packed(weight, weight->scalar_type(), cols);

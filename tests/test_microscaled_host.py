@@ -308,6 +308,27 @@ def test_both_ways_pass_the_same_arguments(record, dtype):
     assert named == set(q._MX_NATIVE) and len(record.seen) % 2 == 0
 
 
+@pytest.mark.parametrize("fmt,block", [(9, 32), (-1, 0), (1, 7)])
+def test_norm_without_codes_looks_at_no_format_and_block(record, fmt, block):
+    """The library does not look at them then; both ways pass them on."""
+    x, w, rstd = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(64), torch.zeros(4)
+    for calls in (record.native, record.refuses):
+        record.library.mx_calls = calls
+        q.quest_rms_norm_mx(x, w, 1e-5, block, fmt, y_out=x.clone(), rstd=rstd)
+    (_, native), (_, general) = record.seen
+    at = record.keep["quest_rms_norm_mx"].argtypes.index(ctypes.c_float)
+    for args in (native, general):
+        assert args[at + 3:at + 8] == (block, fmt, None, None, None)
+    record.library.quest_rms_norm_mx = None                        # native alone
+    record.library.mx_calls = record.native
+    q.quest_rms_norm_mx(x, w, 1e-5, block, fmt, y_out=x.clone())
+    assert len(record.seen) == 3
+    for outputs in (dict(codes=u8(4, 64), scales=u8(4, 2)), dict(codes=u8(4, 32), scales=u8(4, 2))):
+        if fmt not in (0, 1):
+            with pytest.raises(ValueError, match="format"):
+                q.quest_rms_norm_mx(x, w, 1e-5, block, fmt, **outputs)
+
+
 def test_plain_calls_are_native_ones(record):
     for name in q._MX_NATIVE:
         setattr(record.library, name, None)
