@@ -430,6 +430,11 @@ def _packed(t: torch.Tensor | None, name: str, dtype: torch.dtype, shape: tuple)
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape}, got {t.dtype} {tuple(t.shape)}")
 
 
+def _scratch(workspace: torch.Tensor | None) -> None:
+    if workspace is not None and not workspace.is_contiguous():   # (its size is taken to be its memory's)
+        raise ValueError(f"workspace: expected a contiguous tensor, got {tuple(workspace.shape)} with strides {workspace.stride()}")
+
+
 def _code_bytes(fmt: int, cols: int) -> int:
     if fmt not in (QUEST_MX_E2M1, QUEST_MX_E4M3):
         raise ValueError(f"unknown format {fmt}")
@@ -508,6 +513,7 @@ def quest_grad_gemm_mx(which: int, dy: torch.Tensor, q_codes: torch.Tensor, q_sc
         _packed(dy, "dy", torch.bfloat16, (M, N))
         _operand(q_codes, q_scales, None, q_format, M if which == 1 else N, K, "q_")
         _packed(out, "out", torch.bfloat16, (N if which == 1 else M, K))
+        _scratch(workspace)
         _check_devices(dy, q_codes, q_scales, out, workspace)
         status = load().quest_grad_gemm_mx(which, _ptr(dy), _ptr(q_codes), _ptr(q_scales), q_format, M, N, K, _ptr(out),
                                            _ptr(workspace), _bytes(workspace), _stream())
@@ -558,6 +564,7 @@ def quest_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Ten
         _packed(weight, "weight", weight.dtype, (cols,))
         _packed(rstd, "rstd", torch.float32, (rows,))
         _packed(dweight, "dweight", torch.float32, (cols,))
+        _scratch(workspace)
         _check_devices(dy, h, weight, rstd, dh, dx, dweight, workspace)
         status = load().quest_rms_norm_backward(_ptr(dy), _ptr(h), _dtype_code(h), _ptr(weight), _dtype_code(weight),
                                                 _ptr(rstd), _ptr(dh), rows, cols, _ptr(dx), _ptr(dweight), _ptr(workspace),

@@ -403,6 +403,8 @@ public:
         packed(scales, at::kByte, rows, cols / QUEST_MX_GROUP);
         packed(mask, at::kByte, rows, cols / 8);
     }
+    // its size is taken to be its memory's
+    void scratch(const at::Tensor *t) { require(plain && (!t || t->is_contiguous())); }
     // Whether all tensors are on the device whose number `ask_device` returns (tensors in host memory have the number -1)
     void on_device(PyObject *ask_device, std::initializer_list<const at::Tensor *> tensors)
     {
@@ -505,6 +507,7 @@ PyObject *mx_grad_gemm(PyObject *self, PyObject *const *args, Py_ssize_t count)
     r.packed(dy, at::kBFloat16, M, N);
     r.operand(codes, scales, nullptr, format, which == 1 ? M : N, K);
     r.packed(out, at::kBFloat16, which == 1 ? N : M, K);
+    r.scratch(workspace);
     r.on_device(ask_device, {dy, codes, scales, out, workspace});
     QUEST_PLAIN_OR_NONE(r)
     void *pdy = pointer(dy), *po = pointer(out), *pws = pointer(workspace);
@@ -567,6 +570,7 @@ PyObject *mx_rms_norm_backward(PyObject *self, PyObject *const *args, Py_ssize_t
         r.packed(rstd, at::kFloat, rows);
         r.packed(dweight, at::kFloat, cols);
     }
+    r.scratch(workspace);
     r.on_device(ask_device, {dy, h, weight, rstd, dh, dx, dweight, workspace});
     QUEST_PLAIN_OR_NONE(r)
     void *pdy = pointer(dy), *ph = pointer(h), *pw = pointer(weight), *pdh = pointer(dh), *pdx = pointer(dx), *pws = pointer(workspace);

@@ -308,6 +308,19 @@ def test_both_ways_pass_the_same_arguments(record, dtype):
     assert named == set(q._MX_NATIVE) and len(record.seen) % 2 == 0
 
 
+def test_a_workspace_is_as_large_as_it_says(record, monkeypatch):
+    """One whose elements share or skip memory has fewer bytes, or others' among them."""
+    x, w, rstd = torch.zeros(128, 128, dtype=torch.bfloat16), torch.zeros(128), torch.zeros(128)
+    for workspace in (u8(1).expand(1 << 20), u8(1 << 12)[::2], torch.zeros(64, 32).t()):
+        for calls in (record.native, record.refuses):
+            record.library.mx_calls = calls
+            with pytest.raises(ValueError, match="workspace"):
+                q.quest_grad_gemm_mx(0, x, u8(128, 64), u8(128, 4), 0, 128, 128, 128, out=x.clone(), workspace=workspace)
+            with pytest.raises(ValueError, match="workspace"):
+                q.quest_rms_norm_backward(x, x, w, rstd, dx=x.clone(), dweight=w.clone(), workspace=workspace)
+    assert not record.seen
+
+
 @pytest.mark.parametrize("fmt,block", [(9, 32), (-1, 0), (1, 7)])
 def test_norm_without_codes_looks_at_no_format_and_block(record, fmt, block):
     """The library does not look at them then; both ways pass them on."""
