@@ -173,7 +173,7 @@ __global__ __launch_bounds__(backward_threads(GROUP)) void rms_norm_backward_ker
     constexpr int kBlock = backward_threads(GROUP), kGroupThreads = kWave * GROUP, kGroups = kBlock / kGroupThreads;
     constexpr bool kAhead = CH * sizeof(T) <= 8;      // (else the next row's loads would not fit the registers)
     constexpr int kQuads = 8 * (int)sizeof(T) / 16;   // of a chunk
-    extern __shared__ float shares[];                 // [groups][cols], where dweight is wanted
+    extern __shared__ __attribute__((aligned(16))) float shares[];   // [groups][cols], where dweight is wanted
     __shared__ float park[GROUP];
     const int group = threadIdx.x / kGroupThreads, t = threadIdx.x % kGroupThreads;
     float dw[CH][8] = {}, w[CH][8];

@@ -468,6 +468,20 @@ def test_norm_gradient_against_differences():
         assert dw[j] == pytest.approx((loss(h, w + step[1]) - loss(h, w - step[1])) / 2e-6, rel=1e-6, abs=1e-8)
 
 
+def test_workgroup_memory_read_in_16_bytes_is_aligned_to_them():
+    """A dynamic array begins behind the kernel's static ones, at a multiple of its own alignment and no more."""
+    seen = 0
+    for name in sorted(os.listdir(build.CSRC)):
+        text = open(os.path.join(build.CSRC, name)).read()
+        for declared, array in re.findall(r"extern __shared__ (.*?)(\w+)\[\];", text):
+            wide = re.search(r"reinterpret_cast<[^<>]*(?:4|v4f|v4u)\s*\*>\([^;]*\b%s\b" % array, text)
+            wide = wide or re.search(r"(?:load8|store8)\([^;]*\b%s\b" % array, text)
+            if wide:
+                seen += 1
+                assert "aligned(16)" in declared, (name, array)
+    assert seen >= 3
+
+
 # ---- which kernel a product gets
 
 def mx_plan(M, N, K):
