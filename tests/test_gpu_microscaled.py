@@ -509,6 +509,15 @@ def test_norm_backward(rows, cols, dtype, weight_dtype, along):
     assert torch.equal(alone, dx)
 
 
+@pytest.mark.parametrize("rows,cols", [(600, 4096), (300, 2816), (520, 8192), (300, 11008), (257, 16384), (2100, 512), (2051, 1024)])
+@pytest.mark.parametrize("dtype,weight_dtype", [(BF16, F32), (F32, BF16)])
+@pytest.mark.parametrize("along", [True, False])
+def test_norm_backward_of_several_rows_to_a_workgroup(rows, cols, dtype, weight_dtype, along):
+    """More rows than workgroups (256 for rows of more than 2048 elements, 512 of four rows for shorter ones), which do not share them
+    evenly."""
+    test_norm_backward(rows, cols, dtype, weight_dtype, along)
+
+
 def test_norm_backward_against_differences():
     """The gradient of sum(dy * y) against central differences of the 64-bit norm."""
     h, _, w = norm_case(3, 64, F32, F32, 2)
