@@ -482,6 +482,28 @@ def test_workgroup_memory_read_in_16_bytes_is_aligned_to_them():
     assert seen >= 3
 
 
+def test_quest_init_prepares_files_whose_launches_stand_in_headers():
+    """A source file with kernels of its own has one set-up function, which quest_init calls, wherever the launches are written."""
+    def with_headers(name, seen):
+        if name in seen or not os.path.exists(os.path.join(build.CSRC, name)):
+            return ""
+        seen.add(name)
+        text = re.sub(r"//.*", "", open(os.path.join(build.CSRC, name)).read())
+        return text + "".join(with_headers(h, seen) for h in re.findall(r'#include "(\w+\.h)"', text))
+
+    init = open(os.path.join(build.CSRC, "quest_api.hip")).read().split("quest_status quest_init(void)")[1]
+    called = set(re.findall(r"quest::(prepare_\w+)\(\)", init))
+    defined, in_headers = set(), 0
+    for name in build.SOURCES:
+        own = open(os.path.join(build.CSRC, name)).read()
+        if "hipLaunchKernelGGL(" in with_headers(name, set()):
+            setup = re.findall(r"^hipError_t (prepare_\w+_kernels)\(\)", own, flags=re.M)
+            assert len(setup) == 1, f"{name}: set-up functions {setup}"
+            defined.update(setup)
+            in_headers += "hipLaunchKernelGGL(" not in own
+    assert called == defined and in_headers >= 4
+
+
 # ---- which kernel a product gets
 
 def mx_plan(M, N, K):
