@@ -160,7 +160,8 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const T *__restri
         reinterpret_cast<uint32_t *>(mask)[g] = finite ? ~untrusted : 0u;
 }
 
-// Larger blocks: a workgroup holds a row in LDS for the transform's wider strides.
+// Larger blocks: a workgroup holds a row in LDS for the transform's wider strides, three at a time.  Bound by those passes: 16384 x 4096
+// in bf16, blocks of 4096, E2M1 with mask 88 us (blocks of 2048, without LDS, 55; 35 at the rate of a large copy).
 template <typename T, int FORMAT>
 __global__ __launch_bounds__(kThreads) void mx_quantize_row_kernel(const T *__restrict__ x, int cols, int64_t ld, int log2n,
                                                                    float norm, uint8_t *__restrict__ codes,

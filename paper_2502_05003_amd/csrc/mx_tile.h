@@ -89,7 +89,8 @@ enum {
 enum {
     kWholePieces = 0,     // y in 16-byte pieces: rows and columns that fit them
     kAnyRows = 1,         // y of any width, pitch and start
-    kRawSums = 2          // the fp32 sums, and y as above, if it is wanted
+    kRawSums = 2          // the fp32 sums, and y as above, if it is wanted.  (Its three predicated stores for each four sums, beside
+                          // all accumulators, do not fit the registers: 4096 x 4096 x 1024 in E2M1 50 us, y alone 19.)
 };
 
 // TWO: tiles of two stages (else more)
